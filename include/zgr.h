@@ -58,7 +58,7 @@ enum { ZGR_F32 = 0, ZGR_F16 = 1, ZGR_BF16 = 2 };
 enum { ZGR_SCALE_PAPER = 0, ZGR_SCALE_UNIT = 1 };
 
 /* Stream tags of the counter-based generator (fourth counter word). */
-enum { ZGR_TAG_ISO = 0, ZGR_TAG_COEFF = 1 };
+enum { ZGR_TAG_ISO = 0, ZGR_TAG_COEFF = 1, ZGR_TAG_DROPOUT = 2 };
 
 typedef struct zgr_ctx zgr_ctx; /* opaque; created by zgr_init, released by zgr_destroy */
 
@@ -339,6 +339,71 @@ int zgr_device_status(zgr_ctx* ctx, int32_t* code);
 int zgr_get_scalars(const zgr_ctx* ctx, double* a, double* b);
 int zgr_get_state(const zgr_ctx* ctx, int32_t* active, uint64_t* seed, double* net_scale);
 int64_t zgr_launch_count(const zgr_ctx* ctx);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * Operators of the forward pass between two sweeps.  L+ and L- of one query are losses of two forward passes through the perturbed
+ * weights; these calls are the parts of such a pass that need this library's generator and its codes.  They take no context: all
+ * pointers are device pointers of the current device, the work is enqueued on `stream`, and the calls are safe from several threads.  Matrices
+ * are row-major with rows `ld` elements apart (ld >= columns; any alignment of the element size), of one storage type `dtype`
+ * (ZGR_F32, ZGR_F16, ZGR_BF16) for all matrices and vectors of a call.  Arithmetic in fp32, one rounding to the storage type.  An output may be
+ * the very matrix of an input of the same shape (same address, same ld); other overlaps are not allowed.  A call
+ * recorded into a graph repeats its seed on every replay.  No call allocates, and calls that may run at the same time need workspaces of
+ * their own.
+ * ------------------------------------------------------------------------------------------------------------ */
+
+/* Dropout with a mask that is a function of (seed, tensor, row, column) and is never stored, so that the passes for L+ and L-, or a
+ * forward and a backward pass, see the same one:
+ *     y = residual + (keep ? (x + bias) * s : 0),     s = 1 / (1 - p).
+ * p is taken in steps of 2^-16: with t = rint(65536 p), s = 65536 / (65536 - t), an element is dropped with probability t / 65536; p = 1
+ * drops all.  Element (r, c): of generator block r * ceil(cols / 8) + c / 8 of stream (seed, tensor, ZGR_TAG_DROPOUT), 16-bit
+ * half c % 8 (half 0 is the low half of word 0, half 1 its high half, and so on); it is kept if that half is not below t.  The mask
+ * depends on cols, not on ld.  A dropped element contributes exactly nothing, even if it is infinite or NaN.
+ * x, y: rows x cols.  bias: cols, or NULL.  residual: rows x cols, or NULL.  rows or cols may be 0.
+ * ZGR_EINVAL: null or misaligned pointer, negative size, ld below cols, unknown dtype, p outside [0, 1]. */
+int zgr_dropout(const void* x, int64_t ldx, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t rows, int64_t cols,
+                int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* stream);
+
+/* Its backward pass: dx = keep ? dy * s : 0 and, unless dbias is NULL, dbias = column sums of the unrounded dx, in fp32, added in an
+ * order that depends on the sizes alone (repeated calls give identical bits).  The residual's gradient is dy itself.  dx may be dy.
+ * workspace: 16-byte aligned, at least zgr_dropout_backward_workspace(rows, cols) bytes; not used (may be NULL) without dbias.  Its contents
+ * before the call do not matter.  rows = 0 writes zeros into dbias.
+ * ZGR_EINVAL: as zgr_dropout; workspace missing, misaligned or too small. */
+int64_t zgr_dropout_backward_workspace(int64_t rows, int64_t cols);
+int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dbias, int64_t rows, int64_t cols, int32_t dtype, double p,
+                         uint64_t seed, uint32_t tensor, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Rows to signed 8-bit codes with a scale each, x ~ scale * code (the symmetric form of Sec. 3.4, zero point 0; what
+ * zgr_set_coeffs_dtc reads with ldc = cols).  Per row, with a = max |x|:  scale = a / 127, code = rint(x * (127 / a)), where the quotients and
+ * the product are fp32 numbers and rint takes ties to even: codes lie in [-127, 127], and each is within half a step of
+ * x / scale, up to the rounding of the product (2^-16 of a step).  A row with a < 2^-120 gets codes 0 and scale 0, a row that holds an
+ * infinity or a NaN codes 0 and scale NaN.  codes: rows x cols int8, ldc >= cols (nothing between the rows is written).  scales: rows fp32.
+ * ZGR_EINVAL: null or misaligned pointer, cols < 1, rows < 0 or above 2^31 - 1, ld below cols, unknown dtype. */
+int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, int8_t* codes, int64_t ldc, float* scales, void* stream);
+
+/* Linear layer in 8 bits, with a scale for each token and each channel:
+ *     y[t][c] = residual[t][c] + D( (sum_k qx[t][k] w[c][k]) * (sx[t] w_scale[c]) + bias[c] )
+ * qx, sx: the m x k tokens x quantised as by zgr_quantize_rows; w, w_scale: n x k codes and n scales, as zgr_quantize_rows makes them
+ * of the weights (after a sweep: of the perturbed ones).  D is the dropout of zgr_dropout with cols = n (p = 0: nothing).
+ * The sums are exact.  A token that holds an infinity or a NaN gives NaN in its row (where it is not dropped).
+ * w: 16-byte aligned, ldw a multiple of 16 (what lies behind the k-th code of a row is not used).  k at most 2^17.  m may be 0.
+ * workspace: 16-byte aligned, at least zgr_linear_i8_workspace(m, k) bytes (0 for a few tokens, and it may be NULL then): the tokens'
+ * codes and scales.  Its contents before the call do not matter.
+ * ZGR_EINVAL: null or misaligned pointer, size out of range, ld below the row, unknown dtype, p outside [0, 1], workspace missing,
+ * misaligned or too small. */
+int64_t zgr_linear_i8_workspace(int64_t m, int64_t k);
+int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias, const void* residual, int64_t ldr, void* y,
+                  int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* workspace,
+                  int64_t workspace_bytes, void* stream);
+
+/* The same for tokens that are codes already (several layers that read the same tokens quantise them once): x, x_scale as
+ * zgr_quantize_rows makes them, ldx a multiple of 16, x 16-byte aligned.  dtype is that of bias, residual and y. */
+int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
+                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed,
+                  uint32_t tensor, void* stream);
+
+/* Device-side health of the two products on the current device, as zgr_device_status: synchronises and gives the code of the first wait
+ * that gave up since the library was loaded (0 = healthy; the call it belonged to left y unfinished). */
+int zgr_linear_status(int32_t* code);
 
 void zgr_destroy(zgr_ctx* ctx);
 const char* zgr_strerror(int code);

@@ -1,0 +1,380 @@
+// Dropout whose mask is a function of (seed, tensor, row, column) and is never stored, forward and backward.
+//
+//   forward    y  = residual + (keep ? (x + bias) * s : 0)          s = 1 / (1 - p)
+//   backward   dx = keep ? dy * s : 0,   dbias = column sums of dx before it is rounded
+//
+// Arithmetic in fp32, one rounding to the storage type.  A dropped element contributes nothing, whatever it holds: it is selected away,
+// not multiplied by zero.  The bound is memory: x (and residual) read once, y written once; a generator block (about 50 issue slots)
+// serves eight elements.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "zgr.h"
+#include "zgr_forward.cuh"
+#include "zgr_host_internal.h"
+
+namespace zgr {
+
+DropMask make_drop_mask(double p, uint64_t seed, uint32_t tensor) {
+  DropMask m;
+  m.keys = host_make_keys(seed);
+  m.keys.k1[0] ^= ZGR_TAG_DROPOUT;
+  m.tensor = tensor;
+  m.threshold = static_cast<uint32_t>(std::nearbyint(65536.0 * p));
+  m.scale = m.threshold < 65536u ? static_cast<float>(65536.0 / (65536.0 - m.threshold)) : 0.0f;
+  return m;
+}
+
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename T>
+struct DropArgs {
+  const T* x;
+  const T* bias;         // or null
+  const T* residual;     // or null
+  T* y;
+  int64_t rows, cols, ldx, ldr, ldy;
+  int64_t octets;        // per row
+  int64_t total;         // octets in all
+  FastDiv div;           // by `octets` (total < 2^31)
+  int flat;              // 1: rows follow each other without a gap and are whole octets, no bias: octet i lies at element 8 i
+  int group;             // elements that are not on 16-byte boundaries: lanes that share a row (a power of two)
+  DropMask mask;
+};
+
+__device__ __forceinline__ float masked(float v, bool keep, float scale) { return keep ? v * scale : 0.0f; }
+
+// Rows on 16-byte boundaries: a thread takes U octets, kThreads apart, all of its loads in flight before the first block is made.
+// U = 4 for what fills the chip, 1 for the smallest calls, where a thread with four octets is four times as long.
+template <typename T, int U>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs<T> a) {
+  Octet<T> x[U], r[U];
+  int64_t row[U], col[U];
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads * U) + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * kThreads;
+    if (i < a.total) {
+      if (a.flat) {
+        row[u] = 0;
+        col[u] = i * 8;
+      } else {
+        row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.octets;
+        col[u] = (i - row[u] * a.octets) * 8;
+      }
+      if (a.flat || col[u] + 8 <= a.cols) {
+        x[u].load(a.x + row[u] * a.ldx + col[u]);
+        if (a.residual) r[u].load(a.residual + row[u] * a.ldr + col[u]);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * kThreads;
+    if (i >= a.total) return;
+    const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(i));
+    if (a.flat || col[u] + 8 <= a.cols) {
+      float v[8], b[8], add[8];
+      x[u].unpack(v);
+      if (a.bias) {
+        Octet<T> raw;
+        raw.load(a.bias + col[u]);
+        raw.unpack(b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
+      if (a.residual) {
+        r[u].unpack(add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += add[j];
+      }
+      Storage<T>::store8(a.y + row[u] * a.ldy + col[u], v);
+    } else {
+      for (int j = 0; col[u] + j < a.cols; ++j) {      // the end of a row that is not whole octets
+        float v = Storage<T>::load1(a.x + row[u] * a.ldx + col[u] + j);
+        if (a.bias) v += Storage<T>::load1(a.bias + col[u] + j);
+        v = masked(v, keep >> j & 1, a.mask.scale);
+        if (a.residual) v += Storage<T>::load1(a.residual + row[u] * a.ldr + col[u] + j);
+        Storage<T>::store1(a.y + row[u] * a.ldy + col[u] + j, v);
+      }
+    }
+  }
+}
+
+// Rows that start anywhere: a group of G lanes (32, or fewer where a row has fewer octets) takes 8 G elements of a row.  Lane l makes
+// the block of octet l; then lane l serves the elements l, l + G, ... , so that the accesses of a group are contiguous whatever
+// their alignment, and gets the mask of each from the lane that made it.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T> a) {
+  const int lane = threadIdx.x & 31, G = a.group, l = lane & (G - 1);
+  const int64_t per_row = (a.octets + G - 1) / G;                 // groups
+  const int64_t g = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
+  const int64_t row = g / per_row, o0 = (g - row * per_row) * G;
+  const bool inside = row < a.rows;
+  float x[8], r[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int64_t c = o0 * 8 + j * G + l;
+    if (inside && c < a.cols) {
+      x[j] = Storage<T>::load1(a.x + row * a.ldx + c);
+      if (a.bias) x[j] += Storage<T>::load1(a.bias + c);
+      r[j] = a.residual ? Storage<T>::load1(a.residual + row * a.ldr + c) : 0.0f;
+    }
+  }
+  const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int e = j * G + l;
+    const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
+    const int64_t c = o0 * 8 + e;
+    if (inside && c < a.cols) {
+      const float v = masked(x[j], bits >> (e & 7) & 1, a.mask.scale);
+      Storage<T>::store1(a.y + row * a.ldy + c, a.residual ? v + r[j] : v);
+    }
+  }
+}
+
+// The backward pass with the bias's gradient: a block has a strip of 8 G columns and a range of rows, every thread eight fixed columns
+// (an octet, or the elements l, l + G, ... where rows start anywhere) whose sums it keeps in fp32.  The sums of a block meet in shared
+// memory, those of the ranges in the workspace, and column_sums_kernel adds them in a fixed order: the same bits every time.
+constexpr int kRowsInFlight = 4;
+template <typename T, bool OCTETS>
+__global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArgs<T> a, const int64_t rows_per_range, float* __restrict__ partials) {
+  __shared__ float sums[kThreads * 8];
+  const int lane = threadIdx.x & 31, G = a.group, l = threadIdx.x & (G - 1);
+  const int row_lane = threadIdx.x / G, row_lanes = kThreads / G;
+  const int64_t o0 = static_cast<int64_t>(blockIdx.x) * G, c0 = o0 * 8;
+  const int64_t begin = static_cast<int64_t>(blockIdx.y) * rows_per_range, end = min(begin + rows_per_range, a.rows);
+  float acc[8] = {};
+  for (int64_t base = begin; base < end; base += row_lanes * kRowsInFlight) {      // (all lanes of a warp make every trip)
+    if (OCTETS) {
+      const int64_t c = c0 + 8 * l;
+      Octet<T> x[kRowsInFlight];
+#pragma unroll
+      for (int u = 0; u < kRowsInFlight; ++u) {
+        const int64_t row = base + row_lane + u * row_lanes;
+        if (row < end && c + 8 <= a.cols) x[u].load(a.x + row * a.ldx + c);
+      }
+#pragma unroll
+      for (int u = 0; u < kRowsInFlight; ++u) {
+        const int64_t row = base + row_lane + u * row_lanes;
+        if (row < end && c < a.cols) {
+          const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+          if (c + 8 <= a.cols) {
+            float v[8];
+            x[u].unpack(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
+              acc[j] += v[j];
+            }
+            Storage<T>::store8(a.y + row * a.ldy + c, v);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              if (c + j < a.cols) {
+                const float v = masked(Storage<T>::load1(a.x + row * a.ldx + c + j), keep >> j & 1, a.mask.scale);
+                acc[j] += v;
+                Storage<T>::store1(a.y + row * a.ldy + c + j, v);
+              }
+            }
+          }
+        }
+      }
+    } else {
+      for (int u = 0; u < kRowsInFlight; ++u) {
+        const int64_t row = base + row_lane + u * row_lanes;
+        const bool inside = row < end;
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int64_t c = c0 + j * G + l;
+          if (inside && c < a.cols) x[j] = Storage<T>::load1(a.x + row * a.ldx + c);
+        }
+        const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int e = j * G + l;
+          const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
+          const int64_t c = c0 + e;
+          if (inside && c < a.cols) {
+            const float v = masked(x[j], bits >> (e & 7) & 1, a.mask.scale);
+            acc[j] += v;
+            Storage<T>::store1(a.y + row * a.ldy + c, v);
+          }
+        }
+      }
+    }
+  }
+  // sums[row lane][column of the strip]
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[row_lane * (8 * G) + (OCTETS ? 8 * l + j : j * G + l)] = acc[j];
+  __syncthreads();
+  for (int e = threadIdx.x; e < 8 * G; e += kThreads) {
+    if (c0 + e < a.cols) {
+      float t = 0.0f;
+      for (int k = 0; k < row_lanes; ++k) t += sums[k * (8 * G) + e];
+      partials[blockIdx.y * a.cols + c0 + e] = t;
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ partials, int ranges, int64_t cols, T* __restrict__ out) {
+  __shared__ float sums[8][32];
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x;
+  float t = 0.0f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int k = threadIdx.y; k < ranges; k += 8) t += partials[k * cols + c];
+  }
+  sums[threadIdx.y][threadIdx.x] = t;
+  __syncthreads();
+  if (threadIdx.y == 0 && c < cols) {
+    for (int k = 1; k < 8; ++k) t += sums[k][threadIdx.x];
+    Storage<T>::store1(out + c, t);
+  }
+}
+
+// Lanes that share a row: the octets of a row, at most a warp.
+int group_for(int64_t octets) {
+  int g = 1;
+  while (g < 32 && g < octets) g *= 2;
+  return g;
+}
+
+// How the rows of a backward pass with column sums are cut: enough ranges for four blocks on each of the 148 multiprocessors, each of
+// at least one trip.  A function of the sizes alone, so that the sums do not depend on the device.
+struct Ranges {
+  int64_t count, rows;
+};
+Ranges cut_ranges(int64_t rows, int64_t cols) {
+  const int64_t octets = (cols + 7) / 8;
+  const int g = group_for(octets);
+  const int64_t strips = (octets + g - 1) / g, trip = static_cast<int64_t>(kThreads / g) * kRowsInFlight;
+  const int64_t want = std::max<int64_t>(1, 592 / strips), trips = (rows + trip - 1) / trip;
+  Ranges r;
+  r.rows = (trips + std::min(want, trips) - 1) / std::min(want, trips) * trip;
+  r.count = (rows + r.rows - 1) / r.rows;
+  return r;
+}
+
+template <typename T>
+int run_dropout(DropArgs<T> a, cudaStream_t st) {
+  const int size = sizeof(T);
+  a.octets = (a.cols + 7) / 8;
+  a.total = a.rows * a.octets;
+  const bool octets = octets_aligned(a.x, a.rows, a.ldx, size) && octets_aligned(a.y, a.rows, a.ldy, size) &&
+                      (!a.residual || octets_aligned(a.residual, a.rows, a.ldr, size)) && (!a.bias || aligned_to(a.bias, 16));
+  if (octets) {
+    a.flat = a.cols % 8 == 0 && !a.bias && (a.rows == 1 || (a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols)));
+    a.div = make_fast_div(static_cast<uint32_t>(std::min<int64_t>(a.octets, 0x7FFFFFFF)));
+    const bool small = a.total < int64_t{148} * 8 * kThreads;
+    const int64_t blocks = (a.total + kThreads * (small ? 1 : 4) - 1) / (kThreads * (small ? 1 : 4));
+    if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
+    if (small) dropout_kernel<T, 1><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+    else dropout_kernel<T, 4><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+  } else {
+    a.group = group_for(a.octets);
+    const int64_t groups = a.rows * ((a.octets + a.group - 1) / a.group), per_block = kThreads / a.group;
+    const int64_t blocks = (groups + per_block - 1) / per_block;
+    if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
+    dropout_any_kernel<T><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+  }
+  return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+}
+
+template <typename T>
+int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st) {
+  a.octets = (a.cols + 7) / 8;
+  a.total = a.rows * a.octets;
+  a.group = group_for(a.octets);
+  const Ranges r = cut_ranges(a.rows, a.cols);
+  const int64_t strips = (a.octets + a.group - 1) / a.group;
+  if (strips > 0x7FFFFFFF || r.count > 65535) return ZGR_ETOOBIG;
+  const dim3 grid(static_cast<unsigned>(strips), static_cast<unsigned>(r.count));
+  if (octets_aligned(a.x, a.rows, a.ldx, sizeof(T)) && octets_aligned(a.y, a.rows, a.ldy, sizeof(T)))
+    dropout_columns_kernel<T, true><<<grid, kThreads, 0, st>>>(a, r.rows, partials);
+  else
+    dropout_columns_kernel<T, false><<<grid, kThreads, 0, st>>>(a, r.rows, partials);
+  if (cudaGetLastError() != cudaSuccess) return ZGR_ECUDA;
+  column_sums_kernel<T><<<static_cast<unsigned>((a.cols + 31) / 32), dim3(32, 8), 0, st>>>(partials, static_cast<int>(r.count), a.cols, dbias);
+  return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+}
+
+template <typename T>
+DropArgs<T> drop_args(const void* x, int64_t ldx, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t rows, int64_t cols,
+                      const DropMask& mask) {
+  DropArgs<T> a = {};
+  a.x = static_cast<const T*>(x);
+  a.bias = static_cast<const T*>(bias);
+  a.residual = static_cast<const T*>(residual);
+  a.y = static_cast<T*>(y);
+  a.rows = rows;
+  a.cols = cols;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.ldy = ldy;
+  a.mask = mask;
+  return a;
+}
+
+}  // namespace
+}  // namespace zgr
+
+using namespace zgr;
+
+extern "C" {
+
+int zgr_dropout(const void* x, int64_t ldx, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t rows, int64_t cols,
+                int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* stream) {
+  if (!storage_known(dtype) || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return ZGR_EINVAL;
+  if (rows == 0 || cols == 0) return ZGR_OK;
+  const int size = storage_size(dtype);
+  if (!matrix_ok(x, rows, cols, ldx, size) || !matrix_ok(y, rows, cols, ldy, size) || (residual && !matrix_ok(residual, rows, cols, ldr, size)) ||
+      !aligned_to(bias, size))
+    return ZGR_EINVAL;
+  const DropMask mask = make_drop_mask(p, seed, tensor);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch (dtype) {
+    case ZGR_F32: return run_dropout(drop_args<float>(x, ldx, bias, residual, ldr, y, ldy, rows, cols, mask), st);
+    case ZGR_F16: return run_dropout(drop_args<__half>(x, ldx, bias, residual, ldr, y, ldy, rows, cols, mask), st);
+    default: return run_dropout(drop_args<__nv_bfloat16>(x, ldx, bias, residual, ldr, y, ldy, rows, cols, mask), st);
+  }
+}
+
+int64_t zgr_dropout_backward_workspace(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 0) return ZGR_EINVAL;
+  if (rows == 0 || cols == 0) return 0;
+  return cut_ranges(rows, cols).count * cols * static_cast<int64_t>(sizeof(float));
+}
+
+int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dbias, int64_t rows, int64_t cols, int32_t dtype, double p,
+                         uint64_t seed, uint32_t tensor, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!storage_known(dtype) || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return ZGR_EINVAL;
+  const int size = storage_size(dtype);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dbias && !aligned_to(dbias, size)) return ZGR_EINVAL;
+  if (cols == 0) return ZGR_OK;
+  if (rows == 0)      // no rows: the sums are zero
+    return !dbias || cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * size, st) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  if (!matrix_ok(dy, rows, cols, lddy, size) || !matrix_ok(dx, rows, cols, lddx, size)) return ZGR_EINVAL;
+  if (!dbias) return zgr_dropout(dy, lddy, nullptr, nullptr, 0, dx, lddx, rows, cols, dtype, p, seed, tensor, stream);
+  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_dropout_backward_workspace(rows, cols)) return ZGR_EINVAL;
+  const DropMask mask = make_drop_mask(p, seed, tensor);
+  float* partials = static_cast<float*>(workspace);
+  switch (dtype) {
+    case ZGR_F32: return run_backward_bias(drop_args<float>(dy, lddy, nullptr, nullptr, 0, dx, lddx, rows, cols, mask), static_cast<float*>(dbias), partials, st);
+    case ZGR_F16: return run_backward_bias(drop_args<__half>(dy, lddy, nullptr, nullptr, 0, dx, lddx, rows, cols, mask), static_cast<__half*>(dbias), partials, st);
+    default:
+      return run_backward_bias(drop_args<__nv_bfloat16>(dy, lddy, nullptr, nullptr, 0, dx, lddx, rows, cols, mask), static_cast<__nv_bfloat16*>(dbias), partials, st);
+  }
+}
+
+}  // extern "C"

@@ -1,0 +1,107 @@
+// Shared by the operators of the forward pass (dropout, 8-bit product): the counter-based mask and raw access to eight elements.
+#ifndef ZGR_FORWARD_CUH_
+#define ZGR_FORWARD_CUH_
+
+#include "zgr_device.cuh"
+
+namespace zgr {
+
+// A dropout mask as a function of (seed, tensor, row, column).  A row of `cols` elements has O = ceil(cols / 8) generator blocks;
+// block row * O + o decides the elements 8 o .. 8 o + 7, one 16-bit half each.  Every row begins a block of its own, so that the mask
+// knows nothing of strides and alignment, and a tile of a matrix product can make its part of it.  Sixteen bits an element: p in steps
+// of 2^-16 for half the generator's work, which at 32 bits (0.66 cycles an element and scheduler) would be as long as the memory traffic.
+struct DropMask {
+  PhiloxKeys keys;       // with the stream tag folded into the first round's key (it meets that key by xor)
+  uint32_t tensor;
+  uint32_t threshold;    // rint(65536 p): an element is kept if its half is not below; 65536 drops all
+  float scale;           // 65536 / (65536 - threshold): of the probability in effect, so that the expectation is the input
+};
+
+// Host: the mask of (seed, tensor) for a probability in [0, 1].
+DropMask make_drop_mask(double p, uint64_t seed, uint32_t tensor);
+
+// Bit i of the result: element 8 o + i of the row is kept.
+__device__ __forceinline__ uint32_t keep_bits(const DropMask& mask, uint64_t block) {
+  uint32_t x[4];
+  philox_block(block, mask.tensor, 0u, mask.keys, x);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    bits |= ((x[w] & 0xFFFFu) >= mask.threshold ? 1u : 0u) << (2 * w);
+    bits |= ((x[w] >> 16) >= mask.threshold ? 1u : 0u) << (2 * w + 1);
+  }
+  return bits;
+}
+
+// Eight contiguous elements as they lie in memory; conversion when they are used, so that a thread can have several in flight.
+template <typename T>
+struct Octet {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void unpack(float (&v)[8]) const;
+};
+template <>
+__device__ __forceinline__ void Octet<float>::unpack(float (&v)[8]) const {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[4 * i] = __uint_as_float(w[i].x);
+    v[4 * i + 1] = __uint_as_float(w[i].y);
+    v[4 * i + 2] = __uint_as_float(w[i].z);
+    v[4 * i + 3] = __uint_as_float(w[i].w);
+  }
+}
+template <>
+__device__ __forceinline__ void Octet<__half>::unpack(float (&v)[8]) const {
+  const uint32_t r[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+    v[2 * i] = f.x;
+    v[2 * i + 1] = f.y;
+  }
+}
+template <>
+__device__ __forceinline__ void Octet<__nv_bfloat16>::unpack(float (&v)[8]) const {
+  const uint32_t r[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(r[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+  }
+}
+
+// n / d for n < 2^31 by a multiplication (the operands of the launch are fixed, the division is made for every octet).
+struct FastDiv {
+  uint32_t d, mul, shift;
+};
+inline FastDiv make_fast_div(uint32_t d) {
+  uint32_t shift = 0;
+  while ((1ull << shift) < d) ++shift;
+  return FastDiv{d, static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
+}
+__device__ __forceinline__ uint32_t fast_div(uint32_t n, const FastDiv& f) { return (__umulhi(n, f.mul) + n) >> f.shift; }
+
+// ---------------------------------------------------------------------------------------------
+// Host checks that the entry points share.
+// ---------------------------------------------------------------------------------------------
+inline int storage_size(int32_t dtype) { return dtype == 0 ? 4 : 2; }
+inline bool storage_known(int32_t dtype) { return dtype >= 0 && dtype <= 2; }
+inline bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0; }
+// A rows x cols matrix of the storage type with rows `ld` elements apart: no row reaches into the next, offsets stay below 2^62 bytes.
+inline bool matrix_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int size) {
+  if (!p || !aligned_to(p, size)) return false;
+  if (rows > 1 && ld < cols) return false;
+  return ld >= 0 && (rows == 0 || ld <= (int64_t{1} << 60) / rows);
+}
+// Octets of the matrix start on 16-byte boundaries.
+inline bool octets_aligned(const void* p, int64_t rows, int64_t ld, int size) { return aligned_to(p, 16) && (rows <= 1 || ld % (16 / size) == 0); }
+
+}  // namespace zgr
+#endif  // ZGR_FORWARD_CUH_

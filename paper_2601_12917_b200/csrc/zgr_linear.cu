@@ -1,0 +1,756 @@
+// The linear layer of the forward pass in 8 bits: rows quantised with a scale each, the matrix product of two such matrices, and its epilogue.
+//
+//   quantise   a = max_k |x_k|,  scale = a / 127,  code_k = rint(x_k * (127 / a))         per row (a token, or a channel's weights)
+//   product    y[m][n] = residual[m][n] + D( (sum_k qx[m][k] qw[n][k]) * (sx[m] sw[n]) + bias[n] ),   D: dropout, or nothing
+//
+// The sums are 32-bit integers and exact; everything behind them is fp32, rounded once to the storage type.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "zgr.h"
+#include "zgr_forward.cuh"
+#include "zgr_tcgen05.cuh"
+
+namespace zgr {
+namespace {
+
+// Status word of the kernels below (per device; 0 = healthy): where a bounded wait gave up.
+__device__ int g_linear_error = 0;
+
+// ---------------------------------------------------------------------------------------------
+// Rows to codes.  Bound by memory: the row is read once and stays in registers between the two passes over it.
+// ---------------------------------------------------------------------------------------------
+constexpr uint32_t kTinyBits = 0x03800000u;      // 2^-120: a row whose largest magnitude is below it counts as zero (127 / a stays finite)
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+struct RowScale {
+  float scale, inv;
+  bool zero;             // all codes are 0
+};
+// From the largest magnitude's bits.  (Magnitudes as unsigned integers: NaN ranks above infinity, so that one of either shows.)
+__device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {
+  RowScale r;
+  const float a = __uint_as_float(amax_bits);
+  r.zero = amax_bits < kTinyBits || amax_bits >= kInfBits;
+  r.inv = r.zero ? 0.0f : __fdiv_rn(127.0f, a);
+  r.scale = amax_bits < kTinyBits ? 0.0f : (amax_bits >= kInfBits ? __uint_as_float(0x7FC00000u) : __fdiv_rn(a, 127.0f));
+  return r;
+}
+// rint(fl(x inv)) in the low byte: adding 1.5 * 2^23 leaves the nearest integer (ties to even) in the low bits.  The product and the sum
+// are two roundings by definition (not a fused multiply-add).  |x inv| <= 127 (1 + 2^-23), so that no code is above 127.
+__device__ __forceinline__ uint32_t code_of(float x, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12582912.0f)) & 0xFFu; }
+__device__ __forceinline__ uint32_t code4(const float* v, float inv) {
+  const uint32_t a = __float_as_uint(__fadd_rn(__fmul_rn(v[0], inv), 12582912.0f)), b = __float_as_uint(__fadd_rn(__fmul_rn(v[1], inv), 12582912.0f));
+  const uint32_t c = __float_as_uint(__fadd_rn(__fmul_rn(v[2], inv), 12582912.0f)), d = __float_as_uint(__fadd_rn(__fmul_rn(v[3], inv), 12582912.0f));
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Threads per row: WARPS warps; a block has rows for at least four warps.  A thread holds four octets (OCTETS: rows of both matrices on
+// 16-byte and 8-byte boundaries) or 32 single elements, so a row of up to WARPS * 1024 elements is read once.
+template <typename T, int WARPS, bool OCTETS>
+__global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t rows,
+                                                                                     const int cols, int8_t* __restrict__ codes, const int64_t ldc,
+                                                                                     float* __restrict__ scales) {
+  constexpr int kPerRow = WARPS * 32, kRows = WARPS < 4 ? 4 / WARPS : 1;
+  __shared__ uint32_t part[kRows][WARPS];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int t = threadIdx.x % kPerRow, which = threadIdx.x / kPerRow;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + which;
+  const bool inside = row < rows;
+  const T* src = x + row * ldx;
+  Octet<T> raw[4];
+  float one[OCTETS ? 1 : 32];
+  uint32_t amax = 0;
+  if (OCTETS) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (t + i * kPerRow) * 8;
+      raw[i].zero();
+      if (inside && c + 8 <= cols) raw[i].load(src + c);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (t + i * kPerRow) * 8;
+      float v[8];
+      raw[i].unpack(v);
+      if (inside && c < cols && c + 8 > cols)
+        for (int j = 0; c + j < cols; ++j) amax = max(amax, magnitude(Storage<T>::load1(src + c + j)));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = max(amax, magnitude(v[j]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int c = t + i * kPerRow;
+      one[i] = inside && c < cols ? Storage<T>::load1(src + c) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) amax = max(amax, magnitude(one[i]));
+  }
+  amax = __reduce_max_sync(0xFFFFFFFFu, amax);
+  if (WARPS > 1) {
+    if ((threadIdx.x & 31) == 0) part[which][t >> 5] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) amax = max(amax, part[which][w]);
+  }
+  if (!inside) return;
+  const RowScale rs = row_scale(amax);
+  if (t == 0) scales[row] = rs.scale;
+  int8_t* dst = codes + row * ldc;
+  if (OCTETS) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (t + i * kPerRow) * 8;
+      if (c + 8 <= cols) {
+        float v[8];
+        raw[i].unpack(v);
+        *reinterpret_cast<uint2*>(dst + c) = rs.zero ? make_uint2(0, 0) : make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
+      } else {
+        for (int j = 0; c + j < cols; ++j) dst[c + j] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(src + c + j), rs.inv));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int c = t + i * kPerRow;
+      if (c < cols) dst[c] = static_cast<int8_t>(rs.zero ? 0 : code_of(one[i], rs.inv));
+    }
+  }
+}
+
+// Rows of more than 16384 elements: read twice, a block a row.
+template <typename T>
+__global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t cols, int8_t* __restrict__ codes,
+                                                                 const int64_t ldc, float* __restrict__ scales) {
+  __shared__ uint32_t part[16];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t row = blockIdx.x;
+  const T* src = x + row * ldx;
+  uint32_t amax = 0;
+#pragma unroll 8
+  for (int64_t c = threadIdx.x; c < cols; c += 512) amax = max(amax, magnitude(Storage<T>::load1(src + c)));
+  amax = __reduce_max_sync(0xFFFFFFFFu, amax);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) amax = max(amax, part[w]);
+  const RowScale rs = row_scale(amax);
+  if (threadIdx.x == 0) scales[row] = rs.scale;
+#pragma unroll 8
+  for (int64_t c = threadIdx.x; c < cols; c += 512) codes[row * ldc + c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(src + c), rs.inv));
+}
+
+template <typename T, int WARPS>
+void launch_rows(const T* x, int64_t ldx, int64_t rows, int cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  const int per_block = WARPS < 4 ? 4 / WARPS : 1;
+  const unsigned grid = static_cast<unsigned>((rows + per_block - 1) / per_block);
+  const int threads = WARPS < 4 ? 128 : WARPS * 32;
+  if (octets_aligned(x, rows, ldx, sizeof(T)) && aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0))
+    quantize_rows_kernel<T, WARPS, true><<<grid, threads, 0, st>>>(x, ldx, rows, cols, codes, ldc, scales);
+  else
+    quantize_rows_kernel<T, WARPS, false><<<grid, threads, 0, st>>>(x, ldx, rows, cols, codes, ldc, scales);
+}
+
+template <typename T>
+cudaError_t run_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  const T* p = static_cast<const T*>(x);
+  if (cols <= 1024) launch_rows<T, 1>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
+  else if (cols <= 4096) launch_rows<T, 4>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
+  else if (cols <= 8192) launch_rows<T, 8>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
+  else if (cols <= 16384) launch_rows<T, 16>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
+  else quantize_long_rows_kernel<T><<<static_cast<unsigned>(rows), 512, 0, st>>>(p, ldx, cols, codes, ldc, scales);
+  return cudaGetLastError();
+}
+cudaError_t run_quantize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  switch (dtype) {
+    case ZGR_F32: return run_quantize<float>(x, ldx, rows, cols, codes, ldc, scales, st);
+    case ZGR_F16: return run_quantize<__half>(x, ldx, rows, cols, codes, ldc, scales, st);
+    default: return run_quantize<__nv_bfloat16>(x, ldx, rows, cols, codes, ldc, scales, st);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// What the product's kernels share.
+// ---------------------------------------------------------------------------------------------
+struct LinearArgs {
+  const void* x;         // few tokens: m x k in the storage type, quantised by every block for itself
+  int64_t ldx;
+  const float* sx;       // m (product of codes)
+  const int8_t* w;       // n x k codes
+  int64_t ldw;
+  const float* sw;       // n
+  const void* bias;      // n, or null
+  const void* residual;  // m x n, or null
+  int64_t ldr;
+  void* y;               // m x n
+  int64_t ldy;
+  int64_t m, n;
+  int32_t k;
+  DropMask mask;         // threshold 0: nothing is dropped
+};
+
+template <typename T>
+__device__ __forceinline__ float load_one(const void* p, int64_t i) {
+  return Storage<T>::load1(static_cast<const T*>(p) + i);
+}
+
+// One result from its sum.  The rounding of every step is spelled out, so that both kernels give a token the same bits.
+__device__ __forceinline__ float finish1(int sum, float sx, float sw, float bias, float residual, bool keep, float drop_scale, bool drop) {
+  float v = fmaf(static_cast<float>(sum), __fmul_rn(sx, sw), bias);
+  if (drop) v = keep ? __fmul_rn(v, drop_scale) : 0.0f;
+  return __fadd_rn(v, residual);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Few tokens (at most four): the weights are read once and nothing else counts.  A warp takes two channels; its lanes read 16 codes of each
+// at a time, eight loads in flight, and multiply them with the tokens' codes in shared memory (four products an instruction).  Every
+// block quantises the tokens for itself while its first weights are on their way: one launch, no workspace.
+// ---------------------------------------------------------------------------------------------
+constexpr int kFewThreads = 256, kFewChannels = 2, kFewAhead = 4, kFewTokens = 4;
+constexpr int kFewSmem = 96 * 1024;
+
+__device__ __forceinline__ uint4 load_codes16(const int8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
+  acc = __dp4a(static_cast<int>(a.x), static_cast<int>(b.x), acc);
+  acc = __dp4a(static_cast<int>(a.y), static_cast<int>(b.y), acc);
+  acc = __dp4a(static_cast<int>(a.z), static_cast<int>(b.z), acc);
+  return __dp4a(static_cast<int>(a.w), static_cast<int>(b.w), acc);
+}
+
+template <typename T, int M>
+__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArgs a) {
+  extern __shared__ uint4 few_codes[];             // M rows of `chunks` 16-byte pieces, zero behind the last element
+  __shared__ uint32_t part[M][kFewThreads / 32];
+  __shared__ float sx[M];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int whole = a.k / 16, chunks = (a.k + 15) / 16;
+  const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * (kFewThreads / 32) + warp) * kFewChannels;
+  const int8_t* w[kFewChannels];
+#pragma unroll
+  for (int c = 0; c < kFewChannels; ++c) w[c] = a.w + min(n0 + c, a.n - 1) * a.ldw;
+  uint4 ahead[kFewAhead][kFewChannels];
+#pragma unroll
+  for (int i = 0; i < kFewAhead; ++i)
+#pragma unroll
+    for (int c = 0; c < kFewChannels; ++c) {
+      const int ch = lane + 32 * i;
+      ahead[i][c] = ch < whole ? load_codes16(w[c] + ch * 16) : make_uint4(0, 0, 0, 0);
+    }
+  // the tokens' codes
+  const T* x = static_cast<const T*>(a.x);
+  const bool octets = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (M == 1 || a.m == 1 || (a.ldx * sizeof(T) & 15) == 0);
+  uint32_t amax[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    amax[m] = 0;
+    if (m < a.m) {
+      const T* src = x + m * a.ldx;
+      const int full = octets ? a.k / 8 : 0;
+      for (int o = threadIdx.x; o < full; o += kFewThreads) {
+        Octet<T> raw;
+        raw.load(src + o * 8);
+        float v[8];
+        raw.unpack(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax[m] = max(amax[m], magnitude(v[j]));
+      }
+      for (int c = full * 8 + threadIdx.x; c < a.k; c += kFewThreads) amax[m] = max(amax[m], magnitude(Storage<T>::load1(src + c)));
+    }
+    amax[m] = __reduce_max_sync(0xFFFFFFFFu, amax[m]);
+    if (lane == 0) part[m][warp] = amax[m];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kFewThreads / 32; ++i) top = max(top, part[m][i]);
+    const RowScale rs = row_scale(top);
+    if (threadIdx.x == 0) sx[m] = rs.scale;
+    uint2* dst = reinterpret_cast<uint2*>(few_codes + m * chunks);
+    for (int o = threadIdx.x; o < 2 * chunks; o += kFewThreads) {
+      uint2 q = make_uint2(0, 0);
+      if (m < a.m && !rs.zero) {
+        const T* src = x + m * a.ldx + o * 8;
+        float v[8];
+        if (octets && o * 8 + 8 <= a.k) {
+          Octet<T> raw;
+          raw.load(src);
+          raw.unpack(v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = o * 8 + j < a.k ? Storage<T>::load1(src + j) : 0.0f;
+        }
+        q = make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
+      }
+      dst[o] = q;
+    }
+  }
+  __syncthreads();
+  if (n0 >= a.n) return;
+  int acc[kFewChannels][M] = {};
+  for (int base = 0; base < chunks; base += 32 * kFewAhead) {
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i) {
+      const int ch = base + lane + 32 * i;
+      uint4 q[kFewChannels];
+#pragma unroll
+      for (int c = 0; c < kFewChannels; ++c) q[c] = ahead[i][c];
+      const int next = ch + 32 * kFewAhead;
+#pragma unroll
+      for (int c = 0; c < kFewChannels; ++c) ahead[i][c] = next < whole ? load_codes16(w[c] + next * 16) : make_uint4(0, 0, 0, 0);
+      if (ch < chunks) {
+        if (ch >= whole) {                         // the end of the row: nothing behind its last code is read
+#pragma unroll
+          for (int c = 0; c < kFewChannels; ++c) {
+            uint32_t word[4] = {0, 0, 0, 0};
+            for (int j = 0; ch * 16 + j < a.k; ++j) word[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(w[c][ch * 16 + j])) << (8 * (j & 3));
+            q[c] = make_uint4(word[0], word[1], word[2], word[3]);
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const uint4 t = few_codes[m * chunks + ch];
+#pragma unroll
+          for (int c = 0; c < kFewChannels; ++c) acc[c][m] = dot16(q[c], t, acc[c][m]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kFewChannels; ++c)
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const int sum = __reduce_add_sync(0xFFFFFFFFu, acc[c][m]);
+      const int64_t n = n0 + c;
+      if (lane == c * M + m && n < a.n && m < a.m) {
+        const bool drop = a.mask.threshold != 0;
+        const bool keep = drop && (keep_bits(a.mask, static_cast<uint64_t>(m * ((a.n + 7) / 8) + (n >> 3))) >> (n & 7) & 1);
+        const float v = finish1(sum, sx[m], a.sw[n], a.bias ? load_one<T>(a.bias, n) : 0.0f, a.residual ? load_one<T>(a.residual, m * a.ldr + n) : 0.0f,
+                                keep, a.mask.scale, drop);
+        Storage<T>::store1(static_cast<T*>(a.y) + m * a.ldy + n, v);
+      }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// More tokens: tcgen05.  The accumulator's rows are channels, its columns tokens: a tile is 128 channels x `tokens` (16 to 256).  That
+// way round the weights, which are read from memory once, fill the instruction's 128 rows whatever the number of tokens; a thread of the
+// epilogue has one channel (its scale and bias in registers) and a warp writes 32 neighbouring channels of a token at a time,
+// contiguous for every row length.
+// A tile's inner dimension is cut over a cluster of `split` CTAs when there are fewer tiles than multiprocessors.  Integer sums are exact in
+// any order; each CTA leaves its accumulator in its own shared memory and finishes a share of the tokens by reading the others'.
+// ---------------------------------------------------------------------------------------------
+constexpr int kTileChannels = 128, kChunk = 128;           // rows of the weights' box, bytes (= codes) of a stage's rows
+constexpr int kTileThreads = 192;                          // TMA producer, MMA issuer, four epilogue warps
+constexpr int kMaxStages = 12;
+
+struct TileShape {
+  int32_t tokens;        // per tile, a multiple of 16
+  int32_t split;         // CTAs of a cluster that share a tile
+  int32_t stages;
+  int32_t token_tiles;
+};
+
+// kind::i8: signed 8-bit operands, both K-major, 32-bit integer accumulator, M = 128, N = n
+__device__ __forceinline__ uint32_t make_idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+__device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t peer_smem(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ int lds_peer(uint32_t addr) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// Eight tokens of one channel: scale, bias, mask, residual, store.  Lanes of a warp hold 32 consecutive channels from a multiple of 32,
+// eight lanes an octet of the mask: lane j of the eight makes the block of token j, and everyone asks the lane that made it.
+template <typename T, bool DROP>
+__device__ __forceinline__ void finish8(const LinearArgs& a, const int (&sum)[8], int64_t m0, int64_t n, float sw, float bias) {
+  const int lane = threadIdx.x & 31;
+  uint32_t keep = 0xFFu;
+  if (DROP) keep = keep_bits(a.mask, static_cast<uint64_t>((m0 + (lane & 7)) * ((a.n + 7) / 8) + (n >> 3)));
+  float add[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) add[j] = a.residual && n < a.n && m0 + j < a.m ? load_one<T>(a.residual, (m0 + j) * a.ldr + n) : 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t bits = DROP ? __shfl_sync(0xFFFFFFFFu, keep, (lane & 24) | j) : 0u;
+    if (n < a.n && m0 + j < a.m) {
+      const float v = finish1(sum[j], a.sx[m0 + j], sw, bias, add[j], bits >> (lane & 7) & 1, a.mask.scale, DROP);
+      Storage<T>::store1(static_cast<T*>(a.y) + (m0 + j) * a.ldy + n, v);
+    }
+  }
+}
+
+// What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+  }
+}
+
+template <typename T, bool DROP>
+__global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                                                                   const LinearArgs a, const TileShape shape) {
+  extern __shared__ uint8_t tile_smem[];
+  __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  const uint32_t stages0 = (smem_u32(tile_smem) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = shape.split > 1 ? blockIdx.x % shape.split : 0;      // (clusters are consecutive blocks)
+  const int64_t tile = blockIdx.x / shape.split;
+  const int64_t n0 = tile / shape.token_tiles * kTileChannels, m0 = tile % shape.token_tiles * shape.tokens;
+  const int chunks = (a.k + kChunk - 1) / kChunk;
+  const int first = static_cast<int>(static_cast<int64_t>(chunks) * rank / shape.split);
+  const int last = static_cast<int>(static_cast<int64_t>(chunks) * (rank + 1) / shape.split);
+  const uint32_t stage_bytes = kTileChannels * kChunk + shape.tokens * kChunk;
+  const uint32_t tmem_cols = shape.tokens <= 32 ? 32 : (shape.tokens <= 64 ? 64 : (shape.tokens <= 128 ? 128 : 256));
+  volatile int* aborted = &abort_flag;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < shape.stages; ++s) {
+      mbar_init(smem_u32(&full[s]), 1);
+      mbar_init(smem_u32(&empty[s]), 1);
+    }
+    mbar_init(smem_u32(&done), 1);
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&tmem_slot), tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the tokens' codes and scales, and whoever still uses y
+  bool ok = true;
+  if (warp == 0) {
+    if (elect_one()) {
+      int issued = 0;
+      for (int c = first, s = 0, phase = 0; c < last && ok; ++c) {
+        ok = mbar_wait<true>(smem_u32(&empty[s]), phase ^ 1, aborted, &g_linear_error, 101);
+        if (ok) {
+          const uint32_t bar = smem_u32(&full[s]), at = stages0 + s * stage_bytes;
+          mbar_arrive_expect_tx(bar, stage_bytes);
+          tma_load_2d(at, &map_w, c * kChunk, static_cast<int>(n0), bar);
+          tma_load_2d(at + kTileChannels * kChunk, &map_x, c * kChunk, static_cast<int>(m0), bar);
+          ++issued;
+          if (++s == shape.stages) s = 0, phase ^= 1;
+        }
+      }
+      for (int c = max(0, issued - shape.stages); !ok && c < issued; ++c) mbar_drain(smem_u32(&full[c % shape.stages]), c / shape.stages & 1);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (elect_one()) {
+      const uint32_t idesc = make_idesc_i8(kTileChannels, shape.tokens);
+      for (int c = first, s = 0, phase = 0; c < last && ok; ++c) {
+        ok = mbar_wait<true>(smem_u32(&full[s]), phase, aborted, &g_linear_error, 102);
+        if (ok) {
+          tc_fence_after();
+          const uint32_t at = stages0 + s * stage_bytes;
+          const uint64_t wdesc = make_desc(at, kChunk), xdesc = make_desc(at + kTileChannels * kChunk, kChunk);
+#pragma unroll
+          for (int i = 0; i < kChunk / 32; ++i) umma_i8(tmem, wdesc + 2 * i, xdesc + 2 * i, idesc, c > first || i > 0);
+          umma_commit(smem_u32(&empty[s]));
+          if (++s == shape.stages) s = 0, phase ^= 1;
+        }
+      }
+      umma_commit(smem_u32(&done));
+      if (!ok) mbar_drain(smem_u32(&done), 0);
+    }
+    __syncwarp();
+  } else {
+    ok = mbar_wait<false>(smem_u32(&done), 0, aborted, &g_linear_error, 103);
+    ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
+    ok = __all_sync(0xFFFFFFFFu, ok);
+    tc_fence_after();
+  }
+  const int quarter = warp & 3;                             // the lanes of tensor memory that this warp can read
+  const int64_t n = n0 + quarter * 32 + lane;
+  const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+  float sw = 0.0f, bias = 0.0f;
+  if (warp >= 2 && n < a.n) {
+    sw = a.sw[n];
+    if (a.bias) bias = load_one<T>(a.bias, n);
+  }
+  const int groups = shape.tokens / 8;
+  if (shape.split == 1) {
+    if (warp >= 2 && ok) {
+      for (int g = 0; g < groups && m0 + g * 8 < a.m; ++g) {
+        uint32_t v[8];
+        tmem_ld8(mine + g * 8, v);
+        tmem_ld_wait();
+        int sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = static_cast<int>(v[j]);
+        finish8<T, DROP>(a, sum, m0 + g * 8, n, sw, bias);
+      }
+    }
+  } else {
+    // [token][channel], over the stages, which nothing uses any more
+    if (warp >= 2 && ok) {
+      for (int g = 0; g < groups; ++g) {
+        uint32_t v[8];
+        tmem_ld8(mine + g * 8, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sts32(stages0 + ((g * 8 + j) * kTileChannels + quarter * 32 + lane) * 4, v[j]);
+      }
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (warp >= 2) {
+      for (int g = static_cast<int>(rank); g < groups && m0 + g * 8 < a.m; g += shape.split) {
+        int sum[8] = {};
+        for (int r = 0; r < shape.split; ++r) {
+          const uint32_t from = peer_smem(stages0 + (g * 8 * kTileChannels + quarter * 32 + lane) * 4, r);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[j] += lds_peer(from + j * kTileChannels * 4);
+        }
+        finish8<T, DROP>(a, sum, m0 + g * 8, n, sw, bias);
+      }
+    }
+    __syncwarp();
+    cluster_arrive();                                       // no CTA leaves while another reads its sums
+    cluster_wait();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, tmem_cols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Host.
+// ---------------------------------------------------------------------------------------------
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return found ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
+  }();
+  return fn;
+}
+// Rows of codes, k of them, `pitch` bytes apart; a box is box_rows x 128 bytes, swizzled; what lies outside reads as zero.
+bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, int64_t pitch, int box_rows) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(rows > 1 ? pitch : (k + 15) / 16 * 16)};
+  const cuuint32_t box[2] = {kChunk, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t ones[2] = {1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tiles of at most 256 tokens, all of one height; stages for two CTAs on a multiprocessor; as many CTAs a tile as there is room for while
+// each keeps four chunks of the inner dimension.
+constexpr int kTileSmem = 110 * 1024;
+TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
+  TileShape s;
+  s.token_tiles = static_cast<int32_t>((m + 255) / 256);
+  s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
+  s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
+  const int64_t tiles = (n + kTileChannels - 1) / kTileChannels * s.token_tiles, chunks = (k + kChunk - 1) / kChunk;
+  s.split = 1;
+  while (s.split < 8 && tiles * s.split * 2 <= 148 * 2 && chunks / (s.split * 2) >= 4) s.split *= 2;
+  const int stage = (kTileChannels + s.tokens) * kChunk;
+  s.stages = std::min(kMaxStages, (kTileSmem - 1024) / stage);
+  return s;
+}
+int tile_smem_bytes(const TileShape& s) {
+  const int stages = s.stages * (kTileChannels + s.tokens) * kChunk, sums = s.split > 1 ? s.tokens * kTileChannels * 4 : 0;
+  return std::max(stages, sums) + 1024;
+}
+
+template <typename T, bool DROP>
+cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.blockDim = dim3(kTileThreads);
+  cfg.gridDim = dim3(static_cast<unsigned>((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split));
+  cfg.dynamicSmemBytes = static_cast<size_t>(tile_smem_bytes(s));
+  cfg.stream = st;
+  cfg.attrs = attr;
+  if (s.split > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(s.split);
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (behind_quantiser) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, DROP>, mw, mx, a, s);
+}
+
+// Product of codes with the tensor cores.
+int run_product(const int8_t* xq, int64_t ldq, const LinearArgs& a, int32_t dtype, bool behind_quantiser, cudaStream_t st) {
+  const TileShape s = tile_shape(a.m, a.n, a.k);
+  if ((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split > 0x7FFFFFFF) return ZGR_ETOOBIG;
+  CUtensorMap mw, mx;
+  if (!codes_map(&mw, a.w, a.n, a.k, a.ldw, kTileChannels) || !codes_map(&mx, xq, a.m, a.k, ldq, s.tokens)) return ZGR_ECUDA;
+  const bool drop = a.mask.threshold != 0;
+  cudaError_t e;
+  switch (dtype) {
+    case ZGR_F32: e = drop ? launch_tile<float, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<float, false>(mw, mx, a, s, behind_quantiser, st); break;
+    case ZGR_F16: e = drop ? launch_tile<__half, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<__half, false>(mw, mx, a, s, behind_quantiser, st); break;
+    default:
+      e = drop ? launch_tile<__nv_bfloat16, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<__nv_bfloat16, false>(mw, mx, a, s, behind_quantiser, st);
+  }
+  return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+}
+
+template <typename T, int M>
+cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+  if (e != cudaSuccess) return e;
+  const int64_t per_block = kFewThreads / 32 * kFewChannels;
+  linear_few_kernel<T, M><<<static_cast<unsigned>((a.n + per_block - 1) / per_block), kFewThreads, M * ((a.k + 15) / 16) * 16, st>>>(a);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
+  return a.m == 1 ? launch_few<T, 1>(a, st) : (a.m == 2 ? launch_few<T, 2>(a, st) : launch_few<T, kFewTokens>(a, st));
+}
+// Tokens that the kernel for few of them takes: what fits its shared memory, up to four.
+bool few(int64_t m, int64_t k) { return m <= kFewTokens && (m == 1 ? 1 : (m == 2 ? 2 : 4)) * ((k + 15) / 16 * 16) <= kFewSmem; }
+
+constexpr int64_t kMaxInner = 1 << 17;      // 127 * 127 * 2^17 < 2^31: the sums fit 32 bits
+
+// Codes as the products read them: rows on 16-byte boundaries, `ld` below what a tensor map can hold.
+bool codes_ok(const int8_t* p, int64_t rows, int64_t k, int64_t ld) {
+  return matrix_ok(p, rows, k, ld, 1) && aligned_to(p, 16) && (rows <= 1 || (ld % 16 == 0 && ld < (int64_t{1} << 40)));
+}
+
+// Arguments of the product that both entry points check: everything but the tokens.
+bool product_ok(const int8_t* w, int64_t ldw, const float* sw, const void* bias, const void* residual, int64_t ldr, const void* y, int64_t ldy, int64_t m,
+                int64_t n, int64_t k, int32_t dtype, double p) {
+  if (!storage_known(dtype) || m < 0 || n < 1 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF || n > 0x7FFFFFFF || !(p >= 0.0 && p <= 1.0)) return false;
+  if (m == 0) return true;
+  const int size = storage_size(dtype);
+  if (!codes_ok(w, n, k, ldw) || !sw || !aligned_to(sw, 4) || !aligned_to(bias, size)) return false;
+  return matrix_ok(y, m, n, ldy, size) && (!residual || matrix_ok(residual, m, n, ldr, size));
+}
+int64_t padded(int64_t k) { return (k + 15) / 16 * 16; }
+int64_t scales_at(int64_t m, int64_t k) { return (m * padded(k) + 255) / 256 * 256; }
+
+LinearArgs linear_args(const int8_t* w, int64_t ldw, const float* sw, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m,
+                       int64_t n, int64_t k, double p, uint64_t seed, uint32_t tensor) {
+  LinearArgs a = {};
+  a.w = w;
+  a.ldw = ldw;
+  a.sw = sw;
+  a.bias = bias;
+  a.residual = residual;
+  a.ldr = ldr;
+  a.y = y;
+  a.ldy = ldy;
+  a.m = m;
+  a.n = n;
+  a.k = static_cast<int32_t>(k);
+  a.mask = make_drop_mask(p, seed, tensor);
+  return a;
+}
+
+}  // namespace
+}  // namespace zgr
+
+using namespace zgr;
+
+extern "C" {
+
+int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, int8_t* codes, int64_t ldc, float* scales, void* stream) {
+  if (!storage_known(dtype) || rows < 0 || cols < 1 || rows > 0x7FFFFFFF) return ZGR_EINVAL;
+  if (rows == 0) return ZGR_OK;
+  if (!matrix_ok(x, rows, cols, ldx, storage_size(dtype)) || !matrix_ok(codes, rows, cols, ldc, 1) || !scales || !aligned_to(scales, 4)) return ZGR_EINVAL;
+  return run_quantize(dtype, x, ldx, rows, cols, codes, ldc, scales, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+}
+
+int64_t zgr_linear_i8_workspace(int64_t m, int64_t k) {
+  if (m < 0 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF) return ZGR_EINVAL;
+  return few(m, k) ? 0 : scales_at(m, k) + m * static_cast<int64_t>(sizeof(float));
+}
+
+int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias, const void* residual, int64_t ldr, void* y,
+                  int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* workspace,
+                  int64_t workspace_bytes, void* stream) {
+  if (!product_ok(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p)) return ZGR_EINVAL;
+  if (m == 0) return ZGR_OK;
+  if (!matrix_ok(x, m, k, ldx, storage_size(dtype))) return ZGR_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
+  if (few(m, k)) {
+    a.x = x;
+    a.ldx = ldx;
+    const cudaError_t e = dtype == ZGR_F32 ? launch_few<float>(a, st) : (dtype == ZGR_F16 ? launch_few<__half>(a, st) : launch_few<__nv_bfloat16>(a, st));
+    return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  }
+  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_linear_i8_workspace(m, k)) return ZGR_EINVAL;
+  int8_t* codes = static_cast<int8_t*>(workspace);
+  float* scales = reinterpret_cast<float*>(codes + scales_at(m, k));
+  if (run_quantize(dtype, x, ldx, m, k, codes, padded(k), scales, st) != cudaSuccess) return ZGR_ECUDA;
+  a.sx = scales;
+  return run_product(codes, padded(k), a, dtype, true, st);
+}
+
+int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
+                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed,
+                  uint32_t tensor, void* stream) {
+  if (!product_ok(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p)) return ZGR_EINVAL;
+  if (m == 0) return ZGR_OK;
+  if (!codes_ok(x, m, k, ldx) || !x_scale || !aligned_to(x_scale, 4)) return ZGR_EINVAL;
+  LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
+  a.sx = x_scale;
+  return run_product(x, ldx, a, dtype, false, static_cast<cudaStream_t>(stream));
+}
+
+int zgr_linear_status(int32_t* code) {
+  if (!code) return ZGR_EINVAL;
+  if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(code, g_linear_error, sizeof(int)) != cudaSuccess) return ZGR_ECUDA;
+  return ZGR_OK;
+}
+
+}  // extern "C"
