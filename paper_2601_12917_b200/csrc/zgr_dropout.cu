@@ -117,15 +117,15 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T>
   const int64_t g = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
   const int64_t row = g / per_row, o0 = (g - row * per_row) * G;
   const bool inside = row < a.rows;
-  float x[8], r[8];
+  // (Clamped to the matrix, not guarded: a guarded load is a branch with its conversion in it, and the loads then wait for each other.)
+  const int64_t at = min(row, a.rows - 1);
+  T x[8], r[8], b[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int64_t c = o0 * 8 + j * G + l;
-    if (inside && c < a.cols) {
-      x[j] = Storage<T>::load1(a.x + row * a.ldx + c);
-      if (a.bias) x[j] += Storage<T>::load1(a.bias + c);
-      r[j] = a.residual ? Storage<T>::load1(a.residual + row * a.ldr + c) : 0.0f;
-    }
+    const int64_t c = min(o0 * 8 + j * G + l, a.cols - 1);
+    x[j] = a.x[at * a.ldx + c];
+    if (a.residual) r[j] = a.residual[at * a.ldr + c];
+    if (a.bias) b[j] = a.bias[c];
   }
   const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
 #pragma unroll
@@ -133,10 +133,11 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T>
     const int e = j * G + l;
     const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
     const int64_t c = o0 * 8 + e;
-    if (inside && c < a.cols) {
-      const float v = masked(x[j], bits >> (e & 7) & 1, a.mask.scale);
-      Storage<T>::store1(a.y + row * a.ldy + c, a.residual ? v + r[j] : v);
-    }
+    float v = Storage<T>::load1(x + j);
+    if (a.bias) v += Storage<T>::load1(b + j);
+    v = masked(v, bits >> (e & 7) & 1, a.mask.scale);
+    if (a.residual) v += Storage<T>::load1(r + j);
+    if (inside && c < a.cols) Storage<T>::store1(a.y + row * a.ldy + c, v);
   }
 }
 
@@ -191,12 +192,9 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArg
       for (int u = 0; u < kRowsInFlight; ++u) {
         const int64_t row = base + row_lane + u * row_lanes;
         const bool inside = row < end;
-        float x[8];
+        T x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int64_t c = c0 + j * G + l;
-          if (inside && c < a.cols) x[j] = Storage<T>::load1(a.x + row * a.ldx + c);
-        }
+        for (int j = 0; j < 8; ++j) x[j] = a.x[min(row, end - 1) * a.ldx + min(c0 + j * G + l, a.cols - 1)];
         const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -204,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArg
           const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
           const int64_t c = c0 + e;
           if (inside && c < a.cols) {
-            const float v = masked(x[j], bits >> (e & 7) & 1, a.mask.scale);
+            const float v = masked(Storage<T>::load1(x + j), bits >> (e & 7) & 1, a.mask.scale);
             acc[j] += v;
             Storage<T>::store1(a.y + row * a.ldy + c, v);
           }

@@ -60,9 +60,9 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
   const int t = threadIdx.x % kPerRow, which = threadIdx.x / kPerRow;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + which;
   const bool inside = row < rows;
-  const T* src = x + row * ldx;
+  const T* src = x + min(row, rows - 1) * ldx;
   Octet<T> raw[4];
-  float one[OCTETS ? 1 : 32];
+  T one[OCTETS ? 1 : 32];
   uint32_t amax = 0;
   if (OCTETS) {
 #pragma unroll
@@ -84,11 +84,10 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
   } else {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const int c = t + i * kPerRow;
-      one[i] = inside && c < cols ? Storage<T>::load1(src + c) : 0.0f;
+      one[i] = src[min(t + i * kPerRow, cols - 1)];          // (clamped, not guarded: a guarded load is a branch, and they wait for each other)
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) amax = max(amax, magnitude(one[i]));
+    for (int i = 0; i < 32; ++i) amax = max(amax, magnitude(Storage<T>::load1(one + i)));
   }
   amax = __reduce_max_sync(0xFFFFFFFFu, amax);
   if (WARPS > 1) {
@@ -117,7 +116,7 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const int c = t + i * kPerRow;
-      if (c < cols) dst[c] = static_cast<int8_t>(rs.zero ? 0 : code_of(one[i], rs.inv));
+      if (c < cols) dst[c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(one + i), rs.inv));
     }
   }
 }
@@ -325,20 +324,23 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
       }
     }
   }
+  int sum = 0;                                     // lane c * M + m: that of channel c and token m
 #pragma unroll
   for (int c = 0; c < kFewChannels; ++c)
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      const int sum = __reduce_add_sync(0xFFFFFFFFu, acc[c][m]);
-      const int64_t n = n0 + c;
-      if (lane == c * M + m && n < a.n && m < a.m) {
-        const bool drop = a.mask.threshold != 0;
-        const bool keep = drop && (keep_bits(a.mask, static_cast<uint64_t>(m * ((a.n + 7) / 8) + (n >> 3))) >> (n & 7) & 1);
-        const float v = finish1(sum, sx[m], a.sw[n], a.bias ? load_one<T>(a.bias, n) : 0.0f, a.residual ? load_one<T>(a.residual, m * a.ldr + n) : 0.0f,
-                                keep, a.mask.scale, drop);
-        Storage<T>::store1(static_cast<T*>(a.y) + m * a.ldy + n, v);
-      }
+      const int all = __reduce_add_sync(0xFFFFFFFFu, acc[c][m]);
+      if (lane == c * M + m) sum = all;
     }
+  const int m = lane % M;
+  const int64_t n = n0 + lane / M;
+  if (lane < kFewChannels * M && n < a.n && m < a.m) {
+    const bool drop = a.mask.threshold != 0;
+    const bool keep = drop && (keep_bits(a.mask, static_cast<uint64_t>(m * ((a.n + 7) / 8) + (n >> 3))) >> (n & 7) & 1);
+    const float v = finish1(sum, sx[m], a.sw[n], a.bias ? load_one<T>(a.bias, n) : 0.0f, a.residual ? load_one<T>(a.residual, m * a.ldr + n) : 0.0f, keep,
+                            a.mask.scale, drop);
+    Storage<T>::store1(static_cast<T*>(a.y) + m * a.ldy + n, v);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -350,11 +352,12 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
 // any order; each CTA leaves its accumulator in its own shared memory and finishes a share of the tokens by reading the others'.
 // ---------------------------------------------------------------------------------------------
 constexpr int kTileChannels = 128, kChunk = 128;           // rows of the weights' box, bytes (= codes) of a stage's rows
-constexpr int kTileThreads = 192;                          // TMA producer, MMA issuer, four epilogue warps
+constexpr int kTileThreads = 320;                          // TMA producer, MMA issuer, eight epilogue warps
 constexpr int kMaxStages = 12;
 
 struct TileShape {
-  int32_t tokens;        // per tile, a multiple of 16
+  int32_t pair;          // 1: linear_pair_kernel
+  int32_t tokens;        // per tile, a multiple of 16 (of 32 for pairs)
   int32_t split;         // CTAs of a cluster that share a tile
   int32_t stages;
   int32_t token_tiles;
@@ -391,23 +394,50 @@ __device__ __forceinline__ int lds_peer(uint32_t addr) {
   return v;
 }
 
-// Eight tokens of one channel: scale, bias, mask, residual, store.  Lanes of a warp hold 32 consecutive channels from a multiple of 32,
-// eight lanes an octet of the mask: lane j of the eight makes the block of token j, and everyone asks the lane that made it.
-template <typename T, bool DROP>
-__device__ __forceinline__ void finish8(const LinearArgs& a, const int (&sum)[8], int64_t m0, int64_t n, float sw, float bias) {
+// The epilogue of U tokens (8 or 16) of one channel per lane; a warp's lanes hold 32 consecutive channels from a multiple of 32.
+// residual_ahead: the loads, issued before the sums are there.  finish: scales (from shared memory), bias, mask, residual, store; the
+// loads of one batch are never behind the stores of another that they would have to wait for.  Mask: eight lanes share an octet of
+// channels; lane j of the eight makes the block of token j (and 8 + j), and everyone asks the lane that made it.
+// (Addresses are clamped to the matrix instead of the loads being guarded: a guarded load is a branch with its conversion in it, and the
+// loads then wait for each other: 1024 x 2048 outputs behind k = 8192 took 11 us more with a residual than without.)
+template <typename T, int U>
+__device__ __forceinline__ void residual_ahead(const LinearArgs& a, int64_t m0, int64_t n, T (&add)[U]) {
+  const T* p = static_cast<const T*>(a.residual) + min(n, a.n - 1);
+#pragma unroll
+  for (int j = 0; j < U; ++j) add[j] = p[min(m0 + j, a.m - 1) * a.ldr];
+}
+// The scales of the tokens that a warp of the epilogue finishes (the batches of 16 that start at 16 `half`, 32 apart) into its own 128 places: no
+// barrier between warps, so that a warp that gives up a wait leaves nobody behind.
+__device__ __forceinline__ void load_scales(const LinearArgs& a, int64_t m0, int half, int tokens, float* own) {
   const int lane = threadIdx.x & 31;
-  uint32_t keep = 0xFFu;
-  if (DROP) keep = keep_bits(a.mask, static_cast<uint64_t>((m0 + (lane & 7)) * ((a.n + 7) / 8) + (n >> 3)));
-  float add[8];
+  __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) add[j] = a.residual && n < a.n && m0 + j < a.m ? load_one<T>(a.residual, (m0 + j) * a.ldr + n) : 0.0f;
+  for (int i = 0; i < 4; ++i) {
+    const int j = i * 32 + lane, c = (j & 15) + 16 * half + (j >> 4) * 32;
+    if (c < tokens) own[j] = a.sx[min(m0 + c, a.m - 1)];
+  }
+  __syncwarp();
+}
+
+template <typename T, bool DROP, int U>
+__device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum)[U], const float* sx, int64_t m0, int64_t n, float sw, float bias,
+                                       const T (&add)[U]) {
+  const int lane = threadIdx.x & 31;
+  float v[U];
+  uint32_t keep[U / 8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t bits = DROP ? __shfl_sync(0xFFFFFFFFu, keep, (lane & 24) | j) : 0u;
-    if (n < a.n && m0 + j < a.m) {
-      const float v = finish1(sum[j], a.sx[m0 + j], sw, bias, add[j], bits >> (lane & 7) & 1, a.mask.scale, DROP);
-      Storage<T>::store1(static_cast<T*>(a.y) + (m0 + j) * a.ldy + n, v);
-    }
+  for (int h = 0; h < U / 8; ++h)
+    keep[h] = DROP ? keep_bits(a.mask, static_cast<uint64_t>((m0 + 8 * h + (lane & 7)) * ((a.n + 7) / 8) + (n >> 3))) : 0u;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const uint32_t bits = DROP ? __shfl_sync(0xFFFFFFFFu, keep[j / 8], (lane & 24) | (j & 7)) : 0u;
+    v[j] = finish1(static_cast<int>(sum[j]), sx[j], sw, bias, a.residual ? Storage<T>::load1(add + j) : 0.0f, bits >> (lane & 7) & 1, a.mask.scale, DROP);
+  }
+  T* y = static_cast<T*>(a.y) + m0 * a.ldy + n;
+  if (n < a.n) {
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (m0 + j < a.m) Storage<T>::store1(y + j * a.ldy, v[j]);
   }
 }
 
@@ -425,6 +455,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
+  __shared__ float scales[8][128];
   const uint32_t stages0 = (smem_u32(tile_smem) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = shape.split > 1 ? blockIdx.x % shape.split : 0;      // (clusters are consecutive blocks)
@@ -469,7 +500,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
           if (++s == shape.stages) s = 0, phase ^= 1;
         }
       }
-      for (int c = max(0, issued - shape.stages); !ok && c < issued; ++c) mbar_drain(smem_u32(&full[c % shape.stages]), c / shape.stages & 1);
+      // the copies in flight if a wait gave up; else the last commits, which have to land before the CTA leaves
+      for (int c = max(0, issued - shape.stages); c < issued; ++c) mbar_drain(smem_u32(ok ? &empty[c % shape.stages] : &full[c % shape.stages]), c / shape.stages & 1);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -491,37 +523,43 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
       if (!ok) mbar_drain(smem_u32(&done), 0);
     }
     __syncwarp();
-  } else {
+  }
+  // the epilogue's warps: a quarter of the accumulator's rows each, two warps a quarter, which take its batches of tokens in turn
+  const int quarter = warp & 3, half = (warp - 2) >> 2;
+  const int64_t n = n0 + quarter * 32 + lane;
+  const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+  float sw = 0.0f, bias = 0.0f;
+  if (warp >= 2) {
+    load_scales(a, m0, half, shape.tokens, scales[warp - 2]);
+    if (n < a.n) {
+      sw = a.sw[n];
+      if (a.bias) bias = load_one<T>(a.bias, n);
+    }
+    T add[16];
+    if (shape.split == 1 && a.residual) residual_ahead<T, 16>(a, m0 + half * 16, n, add);
     ok = mbar_wait<false>(smem_u32(&done), 0, aborted, &g_linear_error, 103);
     ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
     ok = __all_sync(0xFFFFFFFFu, ok);
     tc_fence_after();
-  }
-  const int quarter = warp & 3;                             // the lanes of tensor memory that this warp can read
-  const int64_t n = n0 + quarter * 32 + lane;
-  const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-  float sw = 0.0f, bias = 0.0f;
-  if (warp >= 2 && n < a.n) {
-    sw = a.sw[n];
-    if (a.bias) bias = load_one<T>(a.bias, n);
-  }
-  const int groups = shape.tokens / 8;
-  if (shape.split == 1) {
-    if (warp >= 2 && ok) {
-      for (int g = 0; g < groups && m0 + g * 8 < a.m; ++g) {
-        uint32_t v[8];
-        tmem_ld8(mine + g * 8, v);
+    if (shape.split == 1 && ok) {
+      for (int c = half * 16; c < shape.tokens && m0 + c < a.m; c += 32) {
+        uint32_t v[16];
+        T next[16];
+        tmem_ld16(mine + c, v);
+        if (a.residual && c + 32 < shape.tokens) residual_ahead<T, 16>(a, m0 + c + 32, n, next);
         tmem_ld_wait();
-        int sum[8];
+        finish<T, DROP, 16>(a, v, scales[warp - 2] + c / 32 * 16, m0 + c, n, sw, bias, add);
+        if (a.residual) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] = static_cast<int>(v[j]);
-        finish8<T, DROP>(a, sum, m0 + g * 8, n, sw, bias);
+          for (int j = 0; j < 16; ++j) add[j] = next[j];
+        }
       }
     }
-  } else {
+  }
+  if (shape.split > 1) {
     // [token][channel], over the stages, which nothing uses any more
     if (warp >= 2 && ok) {
-      for (int g = 0; g < groups; ++g) {
+      for (int g = half; g < shape.tokens / 8; g += 2) {
         uint32_t v[8];
         tmem_ld8(mine + g * 8, v);
         tmem_ld_wait();
@@ -533,14 +571,19 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     cluster_arrive();
     cluster_wait();
     if (warp >= 2) {
-      for (int g = static_cast<int>(rank); g < groups && m0 + g * 8 < a.m; g += shape.split) {
-        int sum[8] = {};
+      for (int g = static_cast<int>(rank) * 2 + half; g < shape.tokens / 8 && m0 + g * 8 < a.m; g += shape.split * 2) {
+        uint32_t sum[8] = {};
+        T add[8];
+        if (a.residual) residual_ahead<T, 8>(a, m0 + g * 8, n, add);
         for (int r = 0; r < shape.split; ++r) {
           const uint32_t from = peer_smem(stages0 + (g * 8 * kTileChannels + quarter * 32 + lane) * 4, r);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) sum[j] += lds_peer(from + j * kTileChannels * 4);
+          for (int j = 0; j < 8; ++j) sum[j] += static_cast<uint32_t>(lds_peer(from + j * kTileChannels * 4));
         }
-        finish8<T, DROP>(a, sum, m0 + g * 8, n, sw, bias);
+        float sx[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sx[j] = a.sx[min(m0 + g * 8 + j, a.m - 1)];
+        finish<T, DROP, 8>(a, sum, sx, m0 + g * 8, n, sw, bias, add);
       }
     }
     __syncwarp();
@@ -552,6 +595,174 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, tmem_cols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Many tokens: the same product by pairs of CTAs (cta_group::2).  A tile is 256 channels x `tokens` (a multiple of 32, at most 256); each
+// CTA of the pair holds 128 of the channels' rows and half of the tokens, so that an operand byte that comes from L2 is used for twice as
+// many products as in linear_tile_kernel.  Pairs stay resident and take tiles in turn; two accumulators of 256 columns: the epilogue
+// of a tile runs beside the products of the next.
+// Barriers: full (of the even CTA) counts the bytes of both CTAs' copies; empty and acc_full are signalled in both CTAs by the even one's
+// commits; acc_empty (of the even CTA) counts the epilogue warps of both.
+// ---------------------------------------------------------------------------------------------
+constexpr int kPairStages = 6, kPairStageBytes = 2 * kTileChannels * kChunk;
+
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const void* tmap, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+               "l"(tmap), "r"(bar), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void umma_i8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(static_cast<uint16_t>(3))
+               : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_dst, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish_pair() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+template <typename T, bool DROP>
+__global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                                                                   const LinearArgs a, const TileShape shape, const int64_t tiles) {
+  extern __shared__ uint8_t pair_smem[];
+  __shared__ __align__(8) uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  __shared__ float scales[8][128];
+  const uint32_t stages0 = (smem_u32(pair_smem) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = blockIdx.x & 1;
+  const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int chunks = (a.k + kChunk - 1) / kChunk;
+  const int half_tokens = shape.tokens / 2;
+  volatile int* aborted = &abort_flag;
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < kPairStages; ++s) {
+      mbar_init(smem_u32(&full[s]), 1);
+      mbar_init(smem_u32(&empty[s]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&acc_full[i]), 1);
+      mbar_init(smem_u32(&acc_empty[i]), 16);
+    }
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the tokens' codes and scales, and whoever still uses y
+  if (warp == 0) {
+    if (elect_one()) {
+      bool ok = true;
+      int issued = 0;
+      for (int64_t t = pair; t < tiles && ok; t += pairs) {
+        const int n0 = static_cast<int>(t / shape.token_tiles * 256 + rank * 128), m0 = static_cast<int>(t % shape.token_tiles * shape.tokens + rank * half_tokens);
+        for (int c = 0; c < chunks && ok; ++c, ++issued) {
+          const int s = issued % kPairStages;
+          ok = mbar_wait<true>(smem_u32(&empty[s]), (issued / kPairStages & 1) ^ 1, aborted, &g_linear_error, 111);
+          if (!ok) break;
+          const uint32_t bar = peer_smem(smem_u32(&full[s]), 0), at = stages0 + s * kPairStageBytes;
+          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * (kTileChannels + half_tokens) * kChunk);
+          tma_load_pair(at, &map_w, c * kChunk, n0, bar);
+          tma_load_pair(at + kTileChannels * kChunk, &map_x, c * kChunk, m0, bar);
+        }
+      }
+      // as in linear_tile_kernel (the even CTA's barriers count the copies of both)
+      for (int c = max(0, issued - kPairStages); c < issued && (ok || rank == 0); ++c)
+        mbar_drain(smem_u32(ok ? &empty[c % kPairStages] : &full[c % kPairStages]), c / kPairStages & 1);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0 && elect_one()) {
+      const uint32_t idesc = make_idesc_i8(256, shape.tokens);
+      bool ok = true;
+      int used = 0, turn = 0;
+      for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
+        const int acc = turn & 1;
+        ok = mbar_wait<true>(smem_u32(&acc_empty[acc]), (turn >> 1 & 1) ^ 1, aborted, &g_linear_error, 112);
+        tc_fence_after();
+        for (int c = 0; c < chunks && ok; ++c, ++used) {
+          const int s = used % kPairStages;
+          ok = mbar_wait<true>(smem_u32(&full[s]), used / kPairStages & 1, aborted, &g_linear_error, 113);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t at = stages0 + s * kPairStageBytes;
+          const uint64_t wdesc = make_desc(at, kChunk), xdesc = make_desc(at + kTileChannels * kChunk, kChunk);
+#pragma unroll
+          for (int i = 0; i < kChunk / 32; ++i) umma_i8_pair(tmem + acc * 256, wdesc + 2 * i, xdesc + 2 * i, idesc, c > 0 || i > 0);
+          umma_commit_pair(smem_u32(&empty[s]));
+        }
+        umma_commit_pair(smem_u32(&acc_full[acc]));
+        if (!ok) mbar_drain(smem_u32(&acc_full[acc]), turn >> 1 & 1);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    bool ok = true;
+    int turn = 0;
+    for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
+      const int acc = turn & 1;
+      const int64_t n = t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, m0 = t % shape.token_tiles * shape.tokens;
+      load_scales(a, m0, half, shape.tokens, scales[warp - 2]);
+      const float sw = n < a.n ? a.sw[n] : 0.0f, bias = a.bias && n < a.n ? load_one<T>(a.bias, n) : 0.0f;
+      T add[16];
+      if (a.residual) residual_ahead<T, 16>(a, m0 + half * 16, n, add);
+      ok = mbar_wait<false>(smem_u32(&acc_full[acc]), turn >> 1 & 1, aborted, &g_linear_error, 114);
+      ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      tc_fence_after();
+      if (ok) {
+        for (int c = half * 16; c < shape.tokens && m0 + c < a.m; c += 32) {
+          uint32_t v[16];
+          T next[16];
+          tmem_ld16(mine + acc * 256 + c, v);
+          if (a.residual && c + 32 < shape.tokens) residual_ahead<T, 16>(a, m0 + c + 32, n, next);
+          tmem_ld_wait();
+          finish<T, DROP, 16>(a, v, scales[warp - 2] + c / 32 * 16, m0 + c, n, sw, bias, add);
+          if (a.residual) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) add[j] = next[j];
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
+      }
+    }
+  }
+  // nobody leaves while the other CTA may still signal its barriers or use its tensor memory
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
   }
 }
 
@@ -581,20 +792,49 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tiles of at most 256 tokens, all of one height; stages for two CTAs on a multiprocessor; as many CTAs a tile as there is room for while
-// each keeps four chunks of the inner dimension.
-constexpr int kTileSmem = 110 * 1024;
+// Kernel, tokens per tile and CTAs per tile: the choice with the shortest estimate.  In cycles of a multiprocessor: operands arrive at about 45
+// bytes a cycle, the tensor cores do 128 * 64 products a cycle, a CTA's set-up and its last batch cost about 2500, a token of the epilogue
+// about 20, sums that travel between CTAs about 1500 and 6 a token.  CTAs beyond one per multiprocessor overlap their set-up and epilogue;
+// pairs overlap all but the last epilogue.
+constexpr int kTileSmem = 110 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
+constexpr double kBytesPerCycle = 45;
 TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
-  TileShape s;
-  s.token_tiles = static_cast<int32_t>((m + 255) / 256);
-  s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
-  s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
-  const int64_t tiles = (n + kTileChannels - 1) / kTileChannels * s.token_tiles, chunks = (k + kChunk - 1) / kChunk;
-  s.split = 1;
-  while (s.split < 8 && tiles * s.split * 2 <= 148 * 2 && chunks / (s.split * 2) >= 4) s.split *= 2;
-  const int stage = (kTileChannels + s.tokens) * kChunk;
-  s.stages = std::min(kMaxStages, (kTileSmem - 1024) / stage);
-  return s;
+  TileShape best = {};
+  double least = 0;
+  const int64_t channel_tiles = (n + kTileChannels - 1) / kTileChannels, chunks = (k + kChunk - 1) / kChunk;
+  for (int64_t most = 256; most >= 16; most /= 2) {
+    TileShape s = {};
+    s.token_tiles = static_cast<int32_t>((m + most - 1) / most);
+    s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
+    s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
+    for (s.split = 1; s.split <= 8 && (s.split == 1 || chunks >= 2 * s.split); s.split *= 2) {
+      const int64_t ctas = channel_tiles * s.token_tiles * s.split, each = (ctas + 147) / 148;
+      const double inner = static_cast<double>((chunks + s.split - 1) / s.split * kChunk);
+      const double steady = std::max(inner * (kTileChannels + s.tokens) / kBytesPerCycle, inner * s.tokens / 64);
+      const double ends = 2500 + 20.0 * s.tokens / s.split + (s.split > 1 ? 1500 + 6.0 * s.tokens : 0);
+      const double cost = steady * each + ends * ((each + 1) / 2);
+      if (best.tokens == 0 || cost < least) {
+        const int stage = (kTileChannels + s.tokens) * kChunk;
+        s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024) / stage);
+        best = s;
+        least = cost;
+      }
+    }
+    if (most >= 64) {
+      s.pair = s.split = 1;
+      s.tokens = (s.tokens + 31) / 32 * 32;
+      s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
+      const int64_t rounds = ((n + 255) / 256 * s.token_tiles + kPairs - 1) / kPairs;
+      const double inner = static_cast<double>(chunks * kChunk);
+      const double steady = std::max(inner * (kTileChannels + s.tokens / 2) / kBytesPerCycle, inner * s.tokens / 64);
+      const double cost = std::max(steady, 20.0 * s.tokens) * rounds + 3500 + 20.0 * s.tokens;
+      if (cost < least) {
+        best = s;
+        least = cost;
+      }
+    }
+  }
+  return best;
 }
 int tile_smem_bytes(const TileShape& s) {
   const int stages = s.stages * (kTileChannels + s.tokens) * kChunk, sums = s.split > 1 ? s.tokens * kTileChannels * 4 : 0;
@@ -603,7 +843,7 @@ int tile_smem_bytes(const TileShape& s) {
 
 template <typename T, bool DROP>
 cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024);
+  cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmemAlone + 1024);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -626,20 +866,47 @@ cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const Line
   return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, DROP>, mw, mx, a, s);
 }
 
+template <typename T, bool DROP>
+cudaError_t launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+  constexpr int smem = kPairStages * kPairStageBytes + 1024;
+  cudaError_t e = cudaFuncSetAttribute(linear_pair_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = (a.n + 255) / 256 * s.token_tiles;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.blockDim = dim3(kTileThreads);
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * std::min<int64_t>(tiles, kPairs)));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.numAttrs = 1;
+  if (behind_quantiser) {
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 2;
+  }
+  return cudaLaunchKernelEx(&cfg, linear_pair_kernel<T, DROP>, mw, mx, a, s, tiles);
+}
+
+template <typename T>
+cudaError_t launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+  const bool drop = a.mask.threshold != 0;
+  if (s.pair) return drop ? launch_pair<T, true>(mw, mx, a, s, behind_quantiser, st) : launch_pair<T, false>(mw, mx, a, s, behind_quantiser, st);
+  return drop ? launch_tile<T, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<T, false>(mw, mx, a, s, behind_quantiser, st);
+}
+
 // Product of codes with the tensor cores.
 int run_product(const int8_t* xq, int64_t ldq, const LinearArgs& a, int32_t dtype, bool behind_quantiser, cudaStream_t st) {
   const TileShape s = tile_shape(a.m, a.n, a.k);
   if ((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split > 0x7FFFFFFF) return ZGR_ETOOBIG;
   CUtensorMap mw, mx;
-  if (!codes_map(&mw, a.w, a.n, a.k, a.ldw, kTileChannels) || !codes_map(&mx, xq, a.m, a.k, ldq, s.tokens)) return ZGR_ECUDA;
-  const bool drop = a.mask.threshold != 0;
-  cudaError_t e;
-  switch (dtype) {
-    case ZGR_F32: e = drop ? launch_tile<float, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<float, false>(mw, mx, a, s, behind_quantiser, st); break;
-    case ZGR_F16: e = drop ? launch_tile<__half, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<__half, false>(mw, mx, a, s, behind_quantiser, st); break;
-    default:
-      e = drop ? launch_tile<__nv_bfloat16, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<__nv_bfloat16, false>(mw, mx, a, s, behind_quantiser, st);
-  }
+  if (!codes_map(&mw, a.w, a.n, a.k, a.ldw, kTileChannels) || !codes_map(&mx, xq, a.m, a.k, ldq, s.pair ? s.tokens / 2 : s.tokens)) return ZGR_ECUDA;
+  const cudaError_t e = dtype == ZGR_F32   ? launch_product<float>(mw, mx, a, s, behind_quantiser, st)
+                        : dtype == ZGR_F16 ? launch_product<__half>(mw, mx, a, s, behind_quantiser, st)
+                                           : launch_product<__nv_bfloat16>(mw, mx, a, s, behind_quantiser, st);
   return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
