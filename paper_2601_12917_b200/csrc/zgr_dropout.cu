@@ -21,6 +21,10 @@ DropMask make_drop_mask(double p, uint64_t seed, uint32_t tensor) {
   DropMask m;
   m.keys = host_make_keys(seed);
   m.keys.k1[0] ^= ZGR_TAG_DROPOUT;
+  const uint64_t first = 0xCD9E8D57ull * tensor, second = 0xD2511F53ull * (static_cast<uint32_t>(first >> 32) ^ m.keys.k0[0]);
+  m.pre.c1 = static_cast<uint32_t>(first) ^ m.keys.k0[1];
+  m.pre.x2 = static_cast<uint32_t>(second >> 32) ^ m.keys.k1[1];
+  m.pre.c3 = static_cast<uint32_t>(second);
   m.tensor = tensor;
   m.threshold = static_cast<uint32_t>(std::nearbyint(65536.0 * p));
   m.scale = m.threshold < 65536u ? static_cast<float>(65536.0 / (65536.0 - m.threshold)) : 0.0f;
@@ -38,76 +42,170 @@ struct DropArgs {
   const T* residual;     // or null
   T* y;
   int64_t rows, cols, ldx, ldr, ldy;
-  int64_t octets;        // per row
-  int64_t total;         // octets in all
-  FastDiv div;           // by `octets` (total < 2^31)
-  int flat;              // 1: rows follow each other without a gap and are whole octets, no bias: octet i lies at element 8 i
-  int group;             // elements that are not on 16-byte boundaries: lanes that share a row (a power of two)
+  int64_t octets;        // generator blocks of a row
+  int64_t pieces;        // eight-element pieces of a row, counted from the 16-byte boundary at or before it
+  int64_t total;         // pieces in all
+  FastDiv div;           // by `pieces` (total < 2^31)
+  int phase;             // elements between that boundary and the first row
+  int bias_octets;       // 1: the bias can be read in octets
+  int group;             // rows of different alignment (dropout_any_kernel) and column sums: lanes that share a row (a power of two)
   DropMask mask;
 };
 
-__device__ __forceinline__ float masked(float v, bool keep, float scale) { return keep ? v * scale : 0.0f; }
+// keep ? v * s : 0.  The element is selected first: what is dropped may be infinite.
+__device__ __forceinline__ float masked(float v, bool keep, float scale) { return (keep ? v : 0.0f) * scale; }
+// ... + residual, one rounding
+__device__ __forceinline__ float masked_plus(float v, bool keep, float scale, float residual) { return fmaf(keep ? v : 0.0f, scale, residual); }
 
-// Rows on 16-byte boundaries: a thread takes U octets, kThreads apart, all of its loads in flight before the first block is made.
-// U = 4 for what fills the chip, 1 for the smallest calls, where a thread with four octets is four times as long.
-template <typename T, int U>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs<T> a) {
+// Rows that start on 16-byte boundaries.  A thread takes U octets, a block's threads apart, all of its loads in flight before the first
+// generator block is made.  U = 4 (2 in fp32) for what fills the chip, 1 for the smallest calls, where a thread with four octets is
+// four times as long.
+// FLAT: the matrices are whole octets without gaps and there is no bias, so that octet i of the tensor lies at element 8 i.
+// What bounds it beside the memory is the number of instructions: an octet may cost about 250 issue slots of its scheduler before they are
+// longer than the traffic of a residual sum, the generator's rounds take 40, and this form needs about 110.
+template <typename T, int U, bool FLAT>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ DropArgs<T> a) {
   Octet<T> x[U], r[U];
-  int64_t row[U], col[U];
+  int64_t at[U], row[U];
+  int col[U];
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads * U) + threadIdx.x;
+  const int cols = static_cast<int>(a.cols);                   // (below 2^31 unless FLAT)
+  const int64_t left = a.total - first;                        // octet u exists if u * kThreads < left
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = first + u * kThreads;
-    if (i < a.total) {
-      if (a.flat) {
-        row[u] = 0;
-        col[u] = i * 8;
+    if (u * kThreads < left) {
+      if (FLAT) {
+        at[u] = (first + u * kThreads) * 8;
+        x[u].load(a.x + at[u]);
+        if (a.residual) r[u].load(a.residual + at[u]);
       } else {
-        row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.octets;
-        col[u] = (i - row[u] * a.octets) * 8;
-      }
-      if (a.flat || col[u] + 8 <= a.cols) {
-        x[u].load(a.x + row[u] * a.ldx + col[u]);
-        if (a.residual) r[u].load(a.residual + row[u] * a.ldr + col[u]);
+        const int64_t i = first + u * kThreads;
+        row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.pieces;
+        col[u] = static_cast<int>(i - row[u] * a.pieces) * 8;
+        if (col[u] + 8 <= cols) {
+          x[u].load(a.x + row[u] * a.ldx + col[u]);
+          if (a.residual) r[u].load(a.residual + row[u] * a.ldr + col[u]);
+        } else {                                               // the end of a row that is not whole octets
+          x[u].gather(a.x + row[u] * a.ldx, col[u], cols);
+          if (a.residual) r[u].gather(a.residual + row[u] * a.ldr, col[u], cols);
+        }
       }
     }
   }
+  const bool none = a.mask.threshold > 65535u;
+  const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = first + u * kThreads;
-    if (i >= a.total) return;
-    const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(i));
-    if (a.flat || col[u] + 8 <= a.cols) {
-      float v[8], b[8], add[8];
+    if (u * kThreads < left) {
+      uint32_t words[4] = {0, 0, 0, 0};
+      const uint64_t block = static_cast<uint64_t>(first + u * kThreads);
+      if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
+      float v[8];
       x[u].unpack(v);
-      if (a.bias) {
+      if (!FLAT && a.bias) {
         Octet<T> raw;
-        raw.load(a.bias + col[u]);
+        float b[8];
+        if (a.bias_octets && col[u] + 8 <= cols) raw.load_shared(a.bias + col[u]);
+        else raw.gather(a.bias, col[u], cols);
         raw.unpack(b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += b[j];
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
       if (a.residual) {
+        float add[8];
         r[u].unpack(add);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += add[j];
+        for (int j = 0; j < 8; ++j) v[j] = masked_plus(v[j], kept(words, j, least), a.mask.scale, add[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = masked(v[j], kept(words, j, least), a.mask.scale);
       }
-      Storage<T>::store8(a.y + row[u] * a.ldy + col[u], v);
-    } else {
-      for (int j = 0; col[u] + j < a.cols; ++j) {      // the end of a row that is not whole octets
-        float v = Storage<T>::load1(a.x + row[u] * a.ldx + col[u] + j);
-        if (a.bias) v += Storage<T>::load1(a.bias + col[u] + j);
-        v = masked(v, keep >> j & 1, a.mask.scale);
-        if (a.residual) v += Storage<T>::load1(a.residual + row[u] * a.ldr + col[u] + j);
-        Storage<T>::store1(a.y + row[u] * a.ldy + col[u] + j, v);
+      if (FLAT) {
+        Storage<T>::store8(a.y + at[u], v);
+      } else {
+        T* y = a.y + row[u] * a.ldy + col[u];
+        if (col[u] + 8 <= cols) {
+          Storage<T>::store8(y, v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (col[u] + j < cols) Storage<T>::store1(y + j, v[j]);
+        }
       }
     }
   }
 }
 
-// Rows that start anywhere: a group of G lanes (32, or fewer where a row has fewer octets) takes 8 G elements of a row.  Lane l makes
+// Rows that do not start on 16-byte boundaries (an odd number of columns), all matrices alike.  A row's pieces of eight elements then begin `s`
+// elements before it, at the boundary, and take the last s bits of one generator block and the first 8 - s of the next: a thread
+// makes the block of its own piece and gets its neighbour's bits from the neighbouring lane; a warp's pieces follow each other, so that only its
+// first lane makes a second block, once for U pieces.
+template <typename T, int U>
+__global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_constant__ DropArgs<T> a) {
+  constexpr int kPhases = 16 / sizeof(T);
+  const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
+  Octet<T> x[U], r[U];
+  int64_t row[U];
+  int piece[U], shift[U];
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = min(first + u * 32, a.total - 1);
+    row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.pieces;
+    piece[u] = static_cast<int>(i - row[u] * a.pieces);
+    shift[u] = static_cast<int>((static_cast<uint32_t>(a.phase) + static_cast<uint32_t>(row[u]) * static_cast<uint32_t>(a.ldx)) & (kPhases - 1));      // (only the low bits count)
+    const int col = piece[u] * 8 - shift[u];
+    if (col >= 0 && col + 8 <= cols) {
+      x[u].load(a.x + row[u] * a.ldx + col);
+      if (a.residual) r[u].load(a.residual + row[u] * a.ldr + col);
+    } else {
+      x[u].gather(a.x + row[u] * a.ldx, col, cols);
+      if (a.residual) r[u].gather(a.residual + row[u] * a.ldr, col, cols);
+    }
+  }
+  uint32_t before = 0;   // lane 31's block of the pieces before
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint64_t block = static_cast<uint64_t>(row[u] * a.octets + piece[u]);
+    const uint32_t own = keep_bits(a.mask, block);
+    uint32_t left = __shfl_up_sync(0xFFFFFFFFu, own, 1);
+    if (lane == 0) left = u > 0 ? before : (piece[u] > 0 ? keep_bits(a.mask, block - 1) : 0u);
+    if (U > 1) before = __shfl_sync(0xFFFFFFFFu, own, 31);
+    const uint32_t keep = (own << 8 | left) >> (8 - shift[u]);
+    if (first + u * 32 < a.total) {
+      const int col = piece[u] * 8 - shift[u];
+      float v[8];
+      x[u].unpack(v);
+      if (a.bias) {
+        Octet<T> raw;
+        float b[8];
+        raw.gather(a.bias, col, cols);
+        raw.unpack(b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+      }
+      if (a.residual) {
+        float add[8];
+        r[u].unpack(add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = masked_plus(v[j], keep >> j & 1, a.mask.scale, add[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
+      }
+      T* y = a.y + row[u] * a.ldy + col;
+      if (col >= 0 && col + 8 <= cols) {
+        Storage<T>::store8(y, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j >= 0 && col + j < cols) Storage<T>::store1(y + j, v[j]);
+      }
+    }
+  }
+}
+
+// Matrices whose rows start at different places of their 16-byte granules: a group of G lanes (32, or fewer where a row has fewer octets) takes 8 G elements of a row.  Lane l makes
 // the block of octet l; then lane l serves the elements l, l + G, ... , so that the accesses of a group are contiguous whatever
 // their alignment, and gets the mask of each from the lane that made it.
 template <typename T>
@@ -135,8 +233,7 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T>
     const int64_t c = o0 * 8 + e;
     float v = Storage<T>::load1(x + j);
     if (a.bias) v += Storage<T>::load1(b + j);
-    v = masked(v, bits >> (e & 7) & 1, a.mask.scale);
-    if (a.residual) v += Storage<T>::load1(r + j);
+    v = masked_plus(v, bits >> (e & 7) & 1, a.mask.scale, a.residual ? Storage<T>::load1(r + j) : 0.0f);
     if (inside && c < a.cols) Storage<T>::store1(a.y + row * a.ldy + c, v);
   }
 }
@@ -151,7 +248,10 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArg
   const int lane = threadIdx.x & 31, G = a.group, l = threadIdx.x & (G - 1);
   const int row_lane = threadIdx.x / G, row_lanes = kThreads / G;
   const int64_t o0 = static_cast<int64_t>(blockIdx.x) * G, c0 = o0 * 8;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // column_sums_kernel, which waits
   const int64_t begin = static_cast<int64_t>(blockIdx.y) * rows_per_range, end = min(begin + rows_per_range, a.rows);
+  const bool none = a.mask.threshold > 65535u;
+  const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
   float acc[8] = {};
   for (int64_t base = begin; base < end; base += row_lanes * kRowsInFlight) {      // (all lanes of a warp make every trip)
     if (OCTETS) {
@@ -166,17 +266,20 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArg
       for (int u = 0; u < kRowsInFlight; ++u) {
         const int64_t row = base + row_lane + u * row_lanes;
         if (row < end && c < a.cols) {
-          const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+          const uint64_t block = static_cast<uint64_t>(row * a.octets + o0 + l);
           if (c + 8 <= a.cols) {
+            uint32_t words[4] = {0, 0, 0, 0};
+            if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
             float v[8];
             x[u].unpack(v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
+              v[j] = masked(v[j], kept(words, j, least), a.mask.scale);
               acc[j] += v[j];
             }
             Storage<T>::store8(a.y + row * a.ldy + c, v);
           } else {
+            const uint32_t keep = keep_bits(a.mask, block);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               if (c + j < a.cols) {
@@ -224,9 +327,10 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArg
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ partials, int ranges, int64_t cols, T* __restrict__ out) {
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* partials, int ranges, int64_t cols, T* out) {
   __shared__ float sums[8][32];
   const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float t = 0.0f;
   if (c < cols) {
 #pragma unroll 8
@@ -258,40 +362,49 @@ Ranges cut_ranges(int64_t rows, int64_t cols) {
   const int64_t strips = (octets + g - 1) / g, trip = static_cast<int64_t>(kThreads / g) * kRowsInFlight;
   const int64_t want = std::max<int64_t>(1, 592 / strips), trips = (rows + trip - 1) / trip;
   Ranges r;
-  r.rows = (trips + std::min(want, trips) - 1) / std::min(want, trips) * trip;
+  const int64_t even = (rows + std::min(want, trips) - 1) / std::min(want, trips), lanes = kThreads / g;
+  r.rows = (even + lanes - 1) / lanes * lanes;
   r.count = (rows + r.rows - 1) / r.rows;
   return r;
 }
 
 template <typename T>
 int run_dropout(DropArgs<T> a, cudaStream_t st) {
-  const int size = sizeof(T);
+  constexpr int size = sizeof(T), kPhases = 16 / size, kMany = sizeof(T) == 2 ? 4 : 2;
   a.octets = (a.cols + 7) / 8;
-  a.total = a.rows * a.octets;
-  const bool octets = octets_aligned(a.x, a.rows, a.ldx, size) && octets_aligned(a.y, a.rows, a.ldy, size) &&
-                      (!a.residual || octets_aligned(a.residual, a.rows, a.ldr, size)) && (!a.bias || aligned_to(a.bias, 16));
-  if (octets) {
-    a.flat = a.cols % 8 == 0 && !a.bias && (a.rows == 1 || (a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols)));
-    a.div = make_fast_div(static_cast<uint32_t>(std::min<int64_t>(a.octets, 0x7FFFFFFF)));
+  a.phase = phase_of(a.x, size);
+  auto alike = [&](const T* p, int64_t ld) { return phase_of(p, size) == a.phase && (a.rows == 1 || (ld - a.ldx) % kPhases == 0); };
+  const bool plain = a.cols % 8 == 0 && a.phase == 0 && !a.bias && (a.rows == 1 || (a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols)));
+  if (alike(a.y, a.ldy) && (!a.residual || alike(a.residual, a.ldr)) && (plain || a.cols < (int64_t{1} << 31) - 64)) {
+    const bool shift = a.phase != 0 || (a.rows > 1 && a.ldx % kPhases != 0);
+    a.pieces = shift ? (a.cols + kPhases - 1 + 7) / 8 : a.octets;
+    a.total = a.rows * a.pieces;
+    a.div = make_fast_div(static_cast<uint32_t>(std::min<int64_t>(a.pieces, 0x7FFFFFFF)));
+    a.bias_octets = aligned_to(a.bias, 16);
+    const bool flat = !shift && plain;
     const bool small = a.total < int64_t{148} * 8 * kThreads;
-    const int64_t blocks = (a.total + kThreads * (small ? 1 : 4) - 1) / (kThreads * (small ? 1 : 4));
+    const int64_t per_block = kThreads * (small ? 1 : kMany), blocks = (a.total + per_block - 1) / per_block;
     if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-    if (small) dropout_kernel<T, 1><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
-    else dropout_kernel<T, 4><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
-  } else {
-    a.group = group_for(a.octets);
-    const int64_t groups = a.rows * ((a.octets + a.group - 1) / a.group), per_block = kThreads / a.group;
-    const int64_t blocks = (groups + per_block - 1) / per_block;
-    if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-    dropout_any_kernel<T><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
+    const unsigned grid = static_cast<unsigned>(blocks);
+    if (shift && small) dropout_shifted_kernel<T, 1><<<grid, kThreads, 0, st>>>(a);
+    else if (shift) dropout_shifted_kernel<T, kMany><<<grid, kThreads, 0, st>>>(a);
+    else if (flat && small) dropout_kernel<T, 1, true><<<grid, kThreads, 0, st>>>(a);
+    else if (flat) dropout_kernel<T, kMany, true><<<grid, kThreads, 0, st>>>(a);
+    else if (small) dropout_kernel<T, 1, false><<<grid, kThreads, 0, st>>>(a);
+    else dropout_kernel<T, kMany, false><<<grid, kThreads, 0, st>>>(a);
+    return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
   }
+  a.group = group_for(a.octets);
+  const int64_t groups = a.rows * ((a.octets + a.group - 1) / a.group), per_block = kThreads / a.group;
+  const int64_t blocks = (groups + per_block - 1) / per_block;
+  if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
+  dropout_any_kernel<T><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
   return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
 template <typename T>
 int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st) {
   a.octets = (a.cols + 7) / 8;
-  a.total = a.rows * a.octets;
   a.group = group_for(a.octets);
   const Ranges r = cut_ranges(a.rows, a.cols);
   const int64_t strips = (a.octets + a.group - 1) / a.group;
@@ -302,8 +415,16 @@ int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st)
   else
     dropout_columns_kernel<T, false><<<grid, kThreads, 0, st>>>(a, r.rows, partials);
   if (cudaGetLastError() != cudaSuccess) return ZGR_ECUDA;
-  column_sums_kernel<T><<<static_cast<unsigned>((a.cols + 31) / 32), dim3(32, 8), 0, st>>>(partials, static_cast<int>(r.count), a.cols, dbias);
-  return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3(static_cast<unsigned>((a.cols + 31) / 32));
+  cfg.blockDim = dim3(32, 8);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  return cudaLaunchKernelEx(&cfg, column_sums_kernel<T>, static_cast<const float*>(partials), static_cast<int>(r.count), a.cols, dbias) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
 template <typename T>

@@ -12,6 +12,7 @@ namespace zgr {
 // of 2^-16 for half the generator's work, which at 32 bits (0.66 cycles an element and scheduler) would be as long as the memory traffic.
 struct DropMask {
   PhiloxKeys keys;       // with the stream tag folded into the first round's key (it meets that key by xor)
+  PhiloxPre pre;         // the part of the first two rounds that is the same for all blocks below 2^32
   uint32_t tensor;
   uint32_t threshold;    // rint(65536 p): an element is kept if its half is not below; 65536 drops all
   float scale;           // 65536 / (65536 - threshold): of the probability in effect, so that the expectation is the input
@@ -20,16 +21,25 @@ struct DropMask {
 // Host: the mask of (seed, tensor) for a probability in [0, 1].
 DropMask make_drop_mask(double p, uint64_t seed, uint32_t tensor);
 
+// The eight halves of a block; element 8 o + i is kept if half i is not below the threshold.  Both halves of a word are compared in its upper
+// half: what lies below the upper half of x decides nothing, because the lower half of keep_least() is zero.
+__device__ __forceinline__ uint32_t keep_least(const DropMask& mask) { return mask.threshold << 16; }      // (threshold below 65536)
+__device__ __forceinline__ void keep_words(const DropMask& mask, uint32_t lo, uint32_t hi, uint32_t (&x)[4]) {
+  if (hi == 0) philox4x32_10_pre(lo, mask.pre, mask.keys, x);
+  else philox4x32_10(lo, hi, mask.tensor, 0u, mask.keys, x);
+}
+__device__ __forceinline__ bool kept(const uint32_t (&x)[4], int i, uint32_t least) { return (i & 1 ? x[i >> 1] : x[i >> 1] << 16) >= least; }
+
 // Bit i of the result: element 8 o + i of the row is kept.
 __device__ __forceinline__ uint32_t keep_bits(const DropMask& mask, uint64_t block) {
+  if (mask.threshold > 65535u) return 0;
   uint32_t x[4];
-  philox_block(block, mask.tensor, 0u, mask.keys, x);
+  keep_words(mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), x);
+  const uint32_t least = keep_least(mask);
   uint32_t bits = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    bits |= ((x[w] & 0xFFFFu) >= mask.threshold ? 1u : 0u) << (2 * w);
-    bits |= ((x[w] >> 16) >= mask.threshold ? 1u : 0u) << (2 * w + 1);
-  }
+  for (int i = 0; i < 8; ++i)
+    if (kept(x, i, least)) bits |= 1u << i;
   return bits;
 }
 
@@ -41,9 +51,21 @@ struct Octet {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
   }
+  // (read again and again, by many threads)
+  __device__ __forceinline__ void load_shared(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
+  // Elements c .. c + 7 of a row of `cols`, of which only some exist (the others are some element of the row).  All loads are issued, none guarded:
+  // a guarded load is a branch, and branches with loads in them wait for each other.
+  __device__ __forceinline__ void gather(const T* row, int c, int cols) {
+    T* e = reinterpret_cast<T*>(w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = row[max(0, min(c + j, cols - 1))];
   }
   __device__ __forceinline__ void unpack(float (&v)[8]) const;
 };
@@ -100,6 +122,8 @@ inline bool matrix_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int
   if (rows > 1 && ld < cols) return false;
   return ld >= 0 && (rows == 0 || ld <= (int64_t{1} << 60) / rows);
 }
+// Elements between a 16-byte boundary and the row; all rows of a matrix have the same if `ld` is a whole number of 16 bytes.
+inline int phase_of(const void* p, int size) { return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / size); }
 // Octets of the matrix start on 16-byte boundaries.
 inline bool octets_aligned(const void* p, int64_t rows, int64_t ld, int size) { return aligned_to(p, 16) && (rows <= 1 || ld % (16 / size) == 0); }
 

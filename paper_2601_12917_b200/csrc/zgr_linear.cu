@@ -48,31 +48,33 @@ __device__ __forceinline__ uint32_t code4(const float* v, float inv) {
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// Threads per row: WARPS warps; a block has rows for at least four warps.  A thread holds four octets (OCTETS: rows of both matrices on
-// 16-byte and 8-byte boundaries) or 32 single elements, so a row of up to WARPS * 1024 elements is read once.
-template <typename T, int WARPS, bool OCTETS>
+// Threads per row: WARPS warps; a block has rows for at least four warps.  A thread holds NV octets (OCTETS: rows of both matrices on
+// 16-byte and 8-byte boundaries) or 8 NV single elements, so a row of up to WARPS * NV * 256 elements is read once.
+// early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not (they could be
+// launched to start early as well and read the codes before they wait).
+template <typename T, int WARPS, int NV, bool OCTETS>
 __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t rows,
                                                                                      const int cols, int8_t* __restrict__ codes, const int64_t ldc,
-                                                                                     float* __restrict__ scales) {
+                                                                                     float* __restrict__ scales, const int early) {
   constexpr int kPerRow = WARPS * 32, kRows = WARPS < 4 ? 4 / WARPS : 1;
   __shared__ uint32_t part[kRows][WARPS];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int t = threadIdx.x % kPerRow, which = threadIdx.x / kPerRow;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + which;
   const bool inside = row < rows;
   const T* src = x + min(row, rows - 1) * ldx;
-  Octet<T> raw[4];
-  T one[OCTETS ? 1 : 32];
+  Octet<T> raw[OCTETS ? NV : 1];
+  T one[OCTETS ? 1 : 8 * NV];
   uint32_t amax = 0;
-  if (OCTETS) {
+  if constexpr (OCTETS) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int c = (t + i * kPerRow) * 8;
       raw[i].zero();
       if (inside && c + 8 <= cols) raw[i].load(src + c);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int c = (t + i * kPerRow) * 8;
       float v[8];
       raw[i].unpack(v);
@@ -83,11 +85,11 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (int i = 0; i < 8 * NV; ++i) {
       one[i] = src[min(t + i * kPerRow, cols - 1)];          // (clamped, not guarded: a guarded load is a branch, and they wait for each other)
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) amax = max(amax, magnitude(Storage<T>::load1(one + i)));
+    for (int i = 0; i < 8 * NV; ++i) amax = max(amax, magnitude(Storage<T>::load1(one + i)));
   }
   amax = __reduce_max_sync(0xFFFFFFFFu, amax);
   if (WARPS > 1) {
@@ -100,9 +102,9 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
   const RowScale rs = row_scale(amax);
   if (t == 0) scales[row] = rs.scale;
   int8_t* dst = codes + row * ldc;
-  if (OCTETS) {
+  if constexpr (OCTETS) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int c = (t + i * kPerRow) * 8;
       if (c + 8 <= cols) {
         float v[8];
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (int i = 0; i < 8 * NV; ++i) {
       const int c = t + i * kPerRow;
       if (c < cols) dst[c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(one + i), rs.inv));
     }
@@ -124,9 +126,9 @@ __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_ke
 // Rows of more than 16384 elements: read twice, a block a row.
 template <typename T>
 __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t cols, int8_t* __restrict__ codes,
-                                                                 const int64_t ldc, float* __restrict__ scales) {
+                                                                 const int64_t ldc, float* __restrict__ scales, const int early) {
   __shared__ uint32_t part[16];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int64_t row = blockIdx.x;
   const T* src = x + row * ldx;
   uint32_t amax = 0;
@@ -143,32 +145,36 @@ __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __rest
   for (int64_t c = threadIdx.x; c < cols; c += 512) codes[row * ldc + c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(src + c), rs.inv));
 }
 
-template <typename T, int WARPS>
-void launch_rows(const T* x, int64_t ldx, int64_t rows, int cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+template <typename T, int WARPS, int NV>
+void launch_rows(const T* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
   const int per_block = WARPS < 4 ? 4 / WARPS : 1;
   const unsigned grid = static_cast<unsigned>((rows + per_block - 1) / per_block);
   const int threads = WARPS < 4 ? 128 : WARPS * 32;
   if (octets_aligned(x, rows, ldx, sizeof(T)) && aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0))
-    quantize_rows_kernel<T, WARPS, true><<<grid, threads, 0, st>>>(x, ldx, rows, cols, codes, ldc, scales);
+    quantize_rows_kernel<T, WARPS, NV, true><<<grid, threads, 0, st>>>(x, ldx, rows, static_cast<int>(cols), codes, ldc, scales, early);
   else
-    quantize_rows_kernel<T, WARPS, false><<<grid, threads, 0, st>>>(x, ldx, rows, cols, codes, ldc, scales);
+    quantize_rows_kernel<T, WARPS, NV, false><<<grid, threads, 0, st>>>(x, ldx, rows, static_cast<int>(cols), codes, ldc, scales, early);
 }
 
 template <typename T>
-cudaError_t run_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+cudaError_t run_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
   const T* p = static_cast<const T*>(x);
-  if (cols <= 1024) launch_rows<T, 1>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
-  else if (cols <= 4096) launch_rows<T, 4>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
-  else if (cols <= 8192) launch_rows<T, 8>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
-  else if (cols <= 16384) launch_rows<T, 16>(p, ldx, rows, static_cast<int>(cols), codes, ldc, scales, st);
-  else quantize_long_rows_kernel<T><<<static_cast<unsigned>(rows), 512, 0, st>>>(p, ldx, cols, codes, ldc, scales);
+  if (cols <= 256) launch_rows<T, 1, 1>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 512) launch_rows<T, 1, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 1024) launch_rows<T, 1, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 2048) launch_rows<T, 4, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 4096) launch_rows<T, 4, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 8192) launch_rows<T, 16, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else if (cols <= 16384) launch_rows<T, 16, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  else quantize_long_rows_kernel<T><<<static_cast<unsigned>(rows), 512, 0, st>>>(p, ldx, cols, codes, ldc, scales, early);
   return cudaGetLastError();
 }
-cudaError_t run_quantize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+cudaError_t run_quantize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early,
+                         cudaStream_t st) {
   switch (dtype) {
-    case ZGR_F32: return run_quantize<float>(x, ldx, rows, cols, codes, ldc, scales, st);
-    case ZGR_F16: return run_quantize<__half>(x, ldx, rows, cols, codes, ldc, scales, st);
-    default: return run_quantize<__nv_bfloat16>(x, ldx, rows, cols, codes, ldc, scales, st);
+    case ZGR_F32: return run_quantize<float>(x, ldx, rows, cols, codes, ldc, scales, early, st);
+    case ZGR_F16: return run_quantize<__half>(x, ldx, rows, cols, codes, ldc, scales, early, st);
+    default: return run_quantize<__nv_bfloat16>(x, ldx, rows, cols, codes, ldc, scales, early, st);
   }
 }
 
@@ -441,6 +447,9 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum
   }
 }
 
+// Waits for the kernel in front: the tokens' codes and scales, the last users of y.
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too.
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
   const unsigned long long t0 = clock64();
@@ -484,17 +493,26 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // the tokens' codes and scales, and whoever still uses y
   bool ok = true;
   if (warp == 0) {
     if (elect_one()) {
+      // The first stages' weights are fetched before the wait for the kernel in front, which is the tokens' quantiser or none: that kernel
+      // writes the workspace only, and it began when everything older was done.
+      const int ahead = min(shape.stages, last - first);
+      for (int s = 0; s < ahead; ++s) {
+        mbar_arrive_expect_tx(smem_u32(&full[s]), stage_bytes);
+        tma_load_2d(stages0 + s * stage_bytes, &map_w, (first + s) * kChunk, static_cast<int>(n0), smem_u32(&full[s]));
+      }
+      dependency_wait();
       int issued = 0;
       for (int c = first, s = 0, phase = 0; c < last && ok; ++c) {
         ok = mbar_wait<true>(smem_u32(&empty[s]), phase ^ 1, aborted, &g_linear_error, 101);
         if (ok) {
           const uint32_t bar = smem_u32(&full[s]), at = stages0 + s * stage_bytes;
-          mbar_arrive_expect_tx(bar, stage_bytes);
-          tma_load_2d(at, &map_w, c * kChunk, static_cast<int>(n0), bar);
+          if (issued >= ahead) {
+            mbar_arrive_expect_tx(bar, stage_bytes);
+            tma_load_2d(at, &map_w, c * kChunk, static_cast<int>(n0), bar);
+          }
           tma_load_2d(at + kTileChannels * kChunk, &map_x, c * kChunk, static_cast<int>(m0), bar);
           ++issued;
           if (++s == shape.stages) s = 0, phase ^= 1;
@@ -530,6 +548,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
   float sw = 0.0f, bias = 0.0f;
   if (warp >= 2) {
+    dependency_wait();
     load_scales(a, m0, half, shape.tokens, scales[warp - 2]);
     if (n < a.n) {
       sw = a.sw[n];
@@ -673,10 +692,16 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
   cluster_wait();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // the tokens' codes and scales, and whoever still uses y
   if (warp == 0) {
     if (elect_one()) {
       bool ok = true;
+      // weights before the wait, as in linear_tile_kernel
+      const int ahead = min(kPairStages, chunks), stage_bytes = (kTileChannels + half_tokens) * kChunk;
+      for (int s = 0; s < ahead; ++s) {
+        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * stage_bytes);
+        tma_load_pair(stages0 + s * kPairStageBytes, &map_w, s * kChunk, static_cast<int>(pair / shape.token_tiles * 256 + rank * 128), peer_smem(smem_u32(&full[s]), 0));
+      }
+      dependency_wait();
       int issued = 0;
       for (int64_t t = pair; t < tiles && ok; t += pairs) {
         const int n0 = static_cast<int>(t / shape.token_tiles * 256 + rank * 128), m0 = static_cast<int>(t % shape.token_tiles * shape.tokens + rank * half_tokens);
@@ -685,8 +710,10 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
           ok = mbar_wait<true>(smem_u32(&empty[s]), (issued / kPairStages & 1) ^ 1, aborted, &g_linear_error, 111);
           if (!ok) break;
           const uint32_t bar = peer_smem(smem_u32(&full[s]), 0), at = stages0 + s * kPairStageBytes;
-          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * (kTileChannels + half_tokens) * kChunk);
-          tma_load_pair(at, &map_w, c * kChunk, n0, bar);
+          if (issued >= ahead) {
+            if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * stage_bytes);
+            tma_load_pair(at, &map_w, c * kChunk, n0, bar);
+          }
           tma_load_pair(at + kTileChannels * kChunk, &map_x, c * kChunk, m0, bar);
         }
       }
@@ -725,6 +752,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
     const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     bool ok = true;
     int turn = 0;
+    dependency_wait();
     for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
       const int acc = turn & 1;
       const int64_t n = t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, m0 = t % shape.token_tiles * shape.tokens;
@@ -792,27 +820,28 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Kernel, tokens per tile and CTAs per tile: the choice with the shortest estimate.  In cycles of a multiprocessor: operands arrive at about 45
-// bytes a cycle, the tensor cores do 128 * 64 products a cycle, a CTA's set-up and its last batch cost about 2500, a token of the epilogue
-// about 20, sums that travel between CTAs about 1500 and 6 a token.  CTAs beyond one per multiprocessor overlap their set-up and epilogue;
-// pairs overlap all but the last epilogue.
+// Kernel, tokens per tile and CTAs per tile: the choice with the shortest estimate, in cycles of a multiprocessor.  From sweeps of all choices
+// at 22 sizes (5 to 8192 tokens, 512 x 512 to 5120 x 13824 and 50265 x 1027 weights): operands arrive at about 70 bytes a cycle, the tensor cores
+// do 128 * 48 products a cycle, a token of the epilogue costs 25 cycles, sums that travel between CTAs 600 a CTA and 12 a token.  One CTA on a
+// multiprocessor with all of its shared memory as stages is better than two, and pairs are better than several rounds of single CTAs.
 constexpr int kTileSmem = 110 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
-constexpr double kBytesPerCycle = 45;
+// copies beside products: the longer of the two, and some of the other (both draw on the same power)
+double overlapped(double a, double b) { return std::max(a, b) + 0.3 * std::min(a, b); }
 TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
   TileShape best = {};
   double least = 0;
   const int64_t channel_tiles = (n + kTileChannels - 1) / kTileChannels, chunks = (k + kChunk - 1) / kChunk;
-  for (int64_t most = 256; most >= 16; most /= 2) {
+  for (int64_t most = 256; most >= 16; most = most == 256 ? 192 : (most == 192 ? 128 : (most == 128 ? 96 : (most == 96 ? 64 : most / 2)))) {
     TileShape s = {};
     s.token_tiles = static_cast<int32_t>((m + most - 1) / most);
     s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
     s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
-    for (s.split = 1; s.split <= 8 && (s.split == 1 || chunks >= 2 * s.split); s.split *= 2) {
+    for (s.split = 1; s.split <= 4 && (s.split == 1 || chunks >= 2 * s.split); s.split *= 2) {
       const int64_t ctas = channel_tiles * s.token_tiles * s.split, each = (ctas + 147) / 148;
       const double inner = static_cast<double>((chunks + s.split - 1) / s.split * kChunk);
-      const double steady = std::max(inner * (kTileChannels + s.tokens) / kBytesPerCycle, inner * s.tokens / 64);
-      const double ends = 2500 + 20.0 * s.tokens / s.split + (s.split > 1 ? 1500 + 6.0 * s.tokens : 0);
-      const double cost = steady * each + ends * ((each + 1) / 2);
+      const double steady = overlapped(inner * (kTileChannels + s.tokens) / 70, inner * s.tokens / 48);
+      const double ends = 3000 + 25.0 * s.tokens / s.split + (s.split > 1 ? 600 * s.split + 12.0 * s.tokens : 0);
+      const double cost = steady * each + ends * ((each + 1) / 2) + (each > 1 ? 1500 : 0);
       if (best.tokens == 0 || cost < least) {
         const int stage = (kTileChannels + s.tokens) * kChunk;
         s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024) / stage);
@@ -826,8 +855,8 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
       s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
       const int64_t rounds = ((n + 255) / 256 * s.token_tiles + kPairs - 1) / kPairs;
       const double inner = static_cast<double>(chunks * kChunk);
-      const double steady = std::max(inner * (kTileChannels + s.tokens / 2) / kBytesPerCycle, inner * s.tokens / 64);
-      const double cost = std::max(steady, 20.0 * s.tokens) * rounds + 3500 + 20.0 * s.tokens;
+      const double steady = overlapped(inner * (kTileChannels + s.tokens / 2) / 70, inner * s.tokens / 48);
+      const double cost = std::max(steady, 25.0 * s.tokens) * rounds + 6500 + 25.0 * s.tokens;
       if (cost < least) {
         best = s;
         least = cost;
@@ -973,7 +1002,7 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
   if (!storage_known(dtype) || rows < 0 || cols < 1 || rows > 0x7FFFFFFF) return ZGR_EINVAL;
   if (rows == 0) return ZGR_OK;
   if (!matrix_ok(x, rows, cols, ldx, storage_size(dtype)) || !matrix_ok(codes, rows, cols, ldc, 1) || !scales || !aligned_to(scales, 4)) return ZGR_EINVAL;
-  return run_quantize(dtype, x, ldx, rows, cols, codes, ldc, scales, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  return run_quantize(dtype, x, ldx, rows, cols, codes, ldc, scales, 0, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
 int64_t zgr_linear_i8_workspace(int64_t m, int64_t k) {
@@ -998,7 +1027,7 @@ int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, cons
   if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_linear_i8_workspace(m, k)) return ZGR_EINVAL;
   int8_t* codes = static_cast<int8_t*>(workspace);
   float* scales = reinterpret_cast<float*>(codes + scales_at(m, k));
-  if (run_quantize(dtype, x, ldx, m, k, codes, padded(k), scales, st) != cudaSuccess) return ZGR_ECUDA;
+  if (run_quantize(dtype, x, ldx, m, k, codes, padded(k), scales, 1, st) != cudaSuccess) return ZGR_ECUDA;
   a.sx = scales;
   return run_product(codes, padded(k), a, dtype, true, st);
 }
