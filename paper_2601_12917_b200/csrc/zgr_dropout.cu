@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
   int col[U];
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads * U) + threadIdx.x;
   const int cols = static_cast<int>(a.cols);                   // (below 2^31 unless FLAT)
+  dependency_wait();
   const int64_t left = a.total - first;                        // octet u exists if u * kThreads < left
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -144,6 +145,7 @@ template <typename T, int U>
 __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_constant__ DropArgs<T> a) {
   constexpr int kPhases = 16 / sizeof(T);
   const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
+  dependency_wait();
   Octet<T> x[U], r[U];
   int64_t row[U];
   int piece[U], shift[U];
@@ -209,12 +211,13 @@ __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_
 // the block of octet l; then lane l serves the elements l, l + G, ... , so that the accesses of a group are contiguous whatever
 // their alignment, and gets the mask of each from the lane that made it.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T> a) {
+__global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_constant__ DropArgs<T> a) {
   const int lane = threadIdx.x & 31, G = a.group, l = lane & (G - 1);
   const int64_t per_row = (a.octets + G - 1) / G;                 // groups
   const int64_t g = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / G;
   const int64_t row = g / per_row, o0 = (g - row * per_row) * G;
   const bool inside = row < a.rows;
+  dependency_wait();
   // (Clamped to the matrix, not guarded: a guarded load is a branch with its conversion in it, and the loads then wait for each other.)
   const int64_t at = min(row, a.rows - 1);
   T x[8], r[8], b[8];
@@ -243,12 +246,13 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const DropArgs<T>
 // memory, those of the ranges in the workspace, and column_sums_kernel adds them in a fixed order: the same bits every time.
 constexpr int kRowsInFlight = 4;
 template <typename T, bool OCTETS>
-__global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const DropArgs<T> a, const int64_t rows_per_range, float* __restrict__ partials) {
+__global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials) {
   __shared__ float sums[kThreads * 8];
   const int lane = threadIdx.x & 31, G = a.group, l = threadIdx.x & (G - 1);
   const int row_lane = threadIdx.x / G, row_lanes = kThreads / G;
   const int64_t o0 = static_cast<int64_t>(blockIdx.x) * G, c0 = o0 * 8;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // column_sums_kernel, which waits
+  dependency_wait();
+  dependents_may_start();      // column_sums_kernel
   const int64_t begin = static_cast<int64_t>(blockIdx.y) * rows_per_range, end = min(begin + rows_per_range, a.rows);
   const bool none = a.mask.threshold > 65535u;
   const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
@@ -330,7 +334,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) column_sums_kernel(const float* partials, int ranges, int64_t cols, T* out) {
   __shared__ float sums[8][32];
   const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  dependency_wait();
   float t = 0.0f;
   if (c < cols) {
 #pragma unroll 8
@@ -385,21 +389,16 @@ int run_dropout(DropArgs<T> a, cudaStream_t st) {
     const bool small = a.total < int64_t{148} * 8 * kThreads;
     const int64_t per_block = kThreads * (small ? 1 : kMany), blocks = (a.total + per_block - 1) / per_block;
     if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-    const unsigned grid = static_cast<unsigned>(blocks);
-    if (shift && small) dropout_shifted_kernel<T, 1><<<grid, kThreads, 0, st>>>(a);
-    else if (shift) dropout_shifted_kernel<T, kMany><<<grid, kThreads, 0, st>>>(a);
-    else if (flat && small) dropout_kernel<T, 1, true><<<grid, kThreads, 0, st>>>(a);
-    else if (flat) dropout_kernel<T, kMany, true><<<grid, kThreads, 0, st>>>(a);
-    else if (small) dropout_kernel<T, 1, false><<<grid, kThreads, 0, st>>>(a);
-    else dropout_kernel<T, kMany, false><<<grid, kThreads, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+    const auto kernel = shift ? (small ? dropout_shifted_kernel<T, 1> : dropout_shifted_kernel<T, kMany>)
+                        : flat ? (small ? dropout_kernel<T, 1, true> : dropout_kernel<T, kMany, true>)
+                               : (small ? dropout_kernel<T, 1, false> : dropout_kernel<T, kMany, false>);
+    return launch_behind(kernel, static_cast<unsigned>(blocks), kThreads, 0, 1, st, a) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
   }
   a.group = group_for(a.octets);
   const int64_t groups = a.rows * ((a.octets + a.group - 1) / a.group), per_block = kThreads / a.group;
   const int64_t blocks = (groups + per_block - 1) / per_block;
   if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-  dropout_any_kernel<T><<<static_cast<unsigned>(blocks), kThreads, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  return launch_behind(dropout_any_kernel<T>, static_cast<unsigned>(blocks), kThreads, 0, 1, st, a) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
 template <typename T>
@@ -410,21 +409,11 @@ int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st)
   const int64_t strips = (a.octets + a.group - 1) / a.group;
   if (strips > 0x7FFFFFFF || r.count > 65535) return ZGR_ETOOBIG;
   const dim3 grid(static_cast<unsigned>(strips), static_cast<unsigned>(r.count));
-  if (octets_aligned(a.x, a.rows, a.ldx, sizeof(T)) && octets_aligned(a.y, a.rows, a.ldy, sizeof(T)))
-    dropout_columns_kernel<T, true><<<grid, kThreads, 0, st>>>(a, r.rows, partials);
-  else
-    dropout_columns_kernel<T, false><<<grid, kThreads, 0, st>>>(a, r.rows, partials);
-  if (cudaGetLastError() != cudaSuccess) return ZGR_ECUDA;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
-  cfg.gridDim = dim3(static_cast<unsigned>((a.cols + 31) / 32));
-  cfg.blockDim = dim3(32, 8);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  return cudaLaunchKernelEx(&cfg, column_sums_kernel<T>, static_cast<const float*>(partials), static_cast<int>(r.count), a.cols, dbias) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
+  const bool octets = octets_aligned(a.x, a.rows, a.ldx, sizeof(T)) && octets_aligned(a.y, a.rows, a.ldy, sizeof(T));
+  if (launch_behind(octets ? dropout_columns_kernel<T, true> : dropout_columns_kernel<T, false>, grid, kThreads, 0, 1, st, a, r.rows, partials) != cudaSuccess)
+    return ZGR_ECUDA;
+  const cudaError_t e = launch_behind(column_sums_kernel<T>, static_cast<unsigned>((a.cols + 31) / 32), dim3(32, 8), 0, 1, st, partials, static_cast<int>(r.count), a.cols, dbias);
+  return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
 template <typename T>

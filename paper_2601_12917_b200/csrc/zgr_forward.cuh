@@ -2,6 +2,8 @@
 #ifndef ZGR_FORWARD_CUH_
 #define ZGR_FORWARD_CUH_
 
+#include <cuda_runtime.h>
+
 #include "zgr_device.cuh"
 
 namespace zgr {
@@ -109,6 +111,35 @@ inline FastDiv make_fast_div(uint32_t d) {
   return FastDiv{d, static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - d)) / d + 1), shift};
 }
 __device__ __forceinline__ uint32_t fast_div(uint32_t n, const FastDiv& f) { return (__umulhi(n, f.mul) + n) >> f.shift; }
+
+// ---------------------------------------------------------------------------------------------
+// Launches.  As the sweeps, every kernel is launched with the programmatic-serialisation attribute and waits for the kernel before it
+// before it touches memory, so that its launch and set-up run beside that kernel's end.  Only a kernel whose successor is the library's own lets
+// it start early, and not before its own wait: what the successor reads ahead of its wait is then older than both.
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  if (cluster > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
 
 // ---------------------------------------------------------------------------------------------
 // Host checks that the entry points share.

@@ -50,15 +50,15 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 
 // Threads per row: WARPS warps; a block has rows for at least four warps.  A thread holds NV octets (OCTETS: rows of both matrices on
 // 16-byte and 8-byte boundaries) or 8 NV single elements, so a row of up to WARPS * NV * 256 elements is read once.
-// early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not (they could be
-// launched to start early as well and read the codes before they wait).
+// early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not.
 template <typename T, int WARPS, int NV, bool OCTETS>
 __global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t rows,
                                                                                      const int cols, int8_t* __restrict__ codes, const int64_t ldc,
                                                                                      float* __restrict__ scales, const int early) {
   constexpr int kPerRow = WARPS * 32, kRows = WARPS < 4 ? 4 / WARPS : 1;
   __shared__ uint32_t part[kRows][WARPS];
-  if (early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  dependency_wait();
+  if (early) dependents_may_start();
   const int t = threadIdx.x % kPerRow, which = threadIdx.x / kPerRow;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + which;
   const bool inside = row < rows;
@@ -128,7 +128,8 @@ template <typename T>
 __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t cols, int8_t* __restrict__ codes,
                                                                  const int64_t ldc, float* __restrict__ scales, const int early) {
   __shared__ uint32_t part[16];
-  if (early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  dependency_wait();
+  if (early) dependents_may_start();
   const int64_t row = blockIdx.x;
   const T* src = x + row * ldx;
   uint32_t amax = 0;
@@ -146,28 +147,25 @@ __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __rest
 }
 
 template <typename T, int WARPS, int NV>
-void launch_rows(const T* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
+cudaError_t launch_rows(const T* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
   const int per_block = WARPS < 4 ? 4 / WARPS : 1;
   const unsigned grid = static_cast<unsigned>((rows + per_block - 1) / per_block);
-  const int threads = WARPS < 4 ? 128 : WARPS * 32;
-  if (octets_aligned(x, rows, ldx, sizeof(T)) && aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0))
-    quantize_rows_kernel<T, WARPS, NV, true><<<grid, threads, 0, st>>>(x, ldx, rows, static_cast<int>(cols), codes, ldc, scales, early);
-  else
-    quantize_rows_kernel<T, WARPS, NV, false><<<grid, threads, 0, st>>>(x, ldx, rows, static_cast<int>(cols), codes, ldc, scales, early);
+  const bool octets = octets_aligned(x, rows, ldx, sizeof(T)) && aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0);
+  return launch_behind(octets ? quantize_rows_kernel<T, WARPS, NV, true> : quantize_rows_kernel<T, WARPS, NV, false>, grid, WARPS < 4 ? 128 : WARPS * 32, 0, 1, st, x, ldx,
+                       rows, static_cast<int>(cols), codes, ldc, scales, early);
 }
 
 template <typename T>
 cudaError_t run_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
   const T* p = static_cast<const T*>(x);
-  if (cols <= 256) launch_rows<T, 1, 1>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 512) launch_rows<T, 1, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 1024) launch_rows<T, 1, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 2048) launch_rows<T, 4, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 4096) launch_rows<T, 4, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 8192) launch_rows<T, 16, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else if (cols <= 16384) launch_rows<T, 16, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  else quantize_long_rows_kernel<T><<<static_cast<unsigned>(rows), 512, 0, st>>>(p, ldx, cols, codes, ldc, scales, early);
-  return cudaGetLastError();
+  if (cols <= 256) return launch_rows<T, 1, 1>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 512) return launch_rows<T, 1, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 1024) return launch_rows<T, 1, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 2048) return launch_rows<T, 4, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 4096) return launch_rows<T, 4, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 8192) return launch_rows<T, 16, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 16384) return launch_rows<T, 16, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  return launch_behind(quantize_long_rows_kernel<T>, static_cast<unsigned>(rows), 512, 0, 1, st, p, ldx, cols, codes, ldc, scales, early);
 }
 cudaError_t run_quantize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early,
                          cudaStream_t st) {
@@ -211,17 +209,20 @@ __device__ __forceinline__ float finish1(int sum, float sx, float sw, float bias
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few tokens (at most four): the weights are read once and nothing else counts.  A warp takes two channels; its lanes read 16 codes of each
-// at a time, eight loads in flight, and multiply them with the tokens' codes in shared memory (four products an instruction).  Every
-// block quantises the tokens for itself while its first weights are on their way: one launch, no workspace.
+// Few tokens (one or two): the weights are read once and nothing else counts.  A block on every multiprocessor; each warp takes channels in turn and
+// streams their codes through slots of its own in shared memory: one lane starts bulk copies of up to 4096 bytes, two to eight of them
+// ahead (about 190 KB in flight on a multiprocessor, whatever the number of registers), all lanes multiply them with the tokens' codes, four
+// products an instruction.  The sums of 32 channels wait in the 32 lanes for one epilogue.  Every block quantises the tokens for itself while its first weights are on their way: one launch, no workspace.
+// With the loads in registers, eight a lane, the issue slots showed (30 to 70 instructions a load): 12.4 us for 4096 -> 11008 and 15.5 us for
+// 11008 -> 4096, 7.0 of them for the bytes.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewThreads = 256, kFewChannels = 2, kFewAhead = 4, kFewTokens = 4;
-constexpr int kFewSmem = 96 * 1024;
+constexpr int kFewThreads = 512, kFewWarps = kFewThreads / 32, kFewTokens = 2, kFewSegment = 4096, kFewSlots = 8;
+constexpr int kFewSmem = 224 * 1024;
+__host__ __device__ constexpr int few_pitch(int k) { return (k + 511) / 512 * 512; }  // bytes of a token's codes: whole steps of 32 lanes
 
-__device__ __forceinline__ uint4 load_codes16(const int8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-  return v;
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
 }
 __device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
   acc = __dp4a(static_cast<int>(a.x), static_cast<int>(b.x), acc);
@@ -229,26 +230,51 @@ __device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
   acc = __dp4a(static_cast<int>(a.z), static_cast<int>(b.z), acc);
   return __dp4a(static_cast<int>(a.w), static_cast<int>(b.w), acc);
 }
+// What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+  }
+}
 
 template <typename T, int M>
-__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArgs a) {
-  extern __shared__ uint4 few_codes[];             // M rows of `chunks` 16-byte pieces, zero behind the last element
-  __shared__ uint32_t part[M][kFewThreads / 32];
+__global__ void __launch_bounds__(kFewThreads, 1) linear_few_kernel(const __grid_constant__ LinearArgs a, const int slots, const int slot_bytes) {
+  extern __shared__ __align__(16) uint8_t few_smem[];   // the warps' slots, then M rows of codes in whole steps, zero from the last whole 16 on
+  __shared__ __align__(8) uint64_t full[kFewWarps][kFewSlots];
+  __shared__ uint32_t part[M][kFewWarps];
   __shared__ float sx[M];
+  __shared__ int8_t rest[M][16];                        // the codes behind the last whole 16
+  __shared__ int abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int whole = a.k / 16, chunks = (a.k + 15) / 16;
-  const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * (kFewThreads / 32) + warp) * kFewChannels;
-  const int8_t* w[kFewChannels];
-#pragma unroll
-  for (int c = 0; c < kFewChannels; ++c) w[c] = a.w + min(n0 + c, a.n - 1) * a.ldw;
-  uint4 ahead[kFewAhead][kFewChannels];
-#pragma unroll
-  for (int i = 0; i < kFewAhead; ++i)
-#pragma unroll
-    for (int c = 0; c < kFewChannels; ++c) {
-      const int ch = lane + 32 * i;
-      ahead[i][c] = ch < whole ? load_codes16(w[c] + ch * 16) : make_uint4(0, 0, 0, 0);
-    }
+  const int whole = a.k / 16 * 16, steps = few_pitch(a.k) / 512, segments = (whole + slot_bytes - 1) / slot_bytes;
+  uint4* codes = reinterpret_cast<uint4*>(few_smem + kFewWarps * slots * slot_bytes);
+  const uint32_t own = smem_u32(few_smem) + warp * slots * slot_bytes;
+  // this warp's channels: first, first + stride, ... (`mine` of them)
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kFewWarps, first = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;
+  const int64_t mine = first < a.n ? (a.n - first + stride - 1) / stride : 0;
+  const int64_t total = mine * segments;                // copies
+  volatile int* aborted = &abort_flag;
+  if (threadIdx.x == 0) abort_flag = 0;
+  int64_t issued = 0;
+  int next_segment = 0, next_slot = 0;
+  const int8_t* next_row = a.w + first * a.ldw;
+  auto issue = [&] {                                    // lane 0
+    const int at = next_segment * slot_bytes, bytes = min(slot_bytes, whole - at);
+    const uint32_t bar = smem_u32(&full[warp][next_slot]);
+    mbar_arrive_expect_tx(bar, bytes);
+    bulk_load(own + next_slot * slot_bytes, next_row + at, bytes, bar);
+    if (++next_slot == slots) next_slot = 0;
+    if (++next_segment == segments) next_segment = 0, next_row += stride * a.ldw;
+    ++issued;
+  };
+  if (lane == 0) {
+    for (int i = 0; i < slots; ++i) mbar_init(smem_u32(&full[warp][i]), 1);
+    fence_mbar_init();
+    dependency_wait();
+    while (issued < total && issued < slots) issue();
+  }
+  __syncwarp();
+  dependency_wait();
   // the tokens' codes
   const T* x = static_cast<const T*>(a.x);
   const bool octets = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (M == 1 || a.m == 1 || (a.ldx * sizeof(T) & 15) == 0);
@@ -258,16 +284,18 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
     amax[m] = 0;
     if (m < a.m) {
       const T* src = x + m * a.ldx;
-      const int full = octets ? a.k / 8 : 0;
-      for (int o = threadIdx.x; o < full; o += kFewThreads) {
+      const int eights = octets ? a.k / 8 : 0;
+#pragma unroll 4
+      for (int o = threadIdx.x; o < eights; o += kFewThreads) {
         Octet<T> raw;
-        raw.load(src + o * 8);
+        raw.load_shared(src + o * 8);
         float v[8];
         raw.unpack(v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) amax[m] = max(amax[m], magnitude(v[j]));
       }
-      for (int c = full * 8 + threadIdx.x; c < a.k; c += kFewThreads) amax[m] = max(amax[m], magnitude(Storage<T>::load1(src + c)));
+#pragma unroll 4
+      for (int c = eights * 8 + threadIdx.x; c < a.k; c += kFewThreads) amax[m] = max(amax[m], magnitude(Storage<T>::load1(src + c)));
     }
     amax[m] = __reduce_max_sync(0xFFFFFFFFu, amax[m]);
     if (lane == 0) part[m][warp] = amax[m];
@@ -277,76 +305,92 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const LinearArg
   for (int m = 0; m < M; ++m) {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kFewThreads / 32; ++i) top = max(top, part[m][i]);
+    for (int i = 0; i < kFewWarps; ++i) top = max(top, part[m][i]);
     const RowScale rs = row_scale(top);
     if (threadIdx.x == 0) sx[m] = rs.scale;
-    uint2* dst = reinterpret_cast<uint2*>(few_codes + m * chunks);
-    for (int o = threadIdx.x; o < 2 * chunks; o += kFewThreads) {
+    const T* src = x + m * a.ldx;
+    const bool some = m < a.m && !rs.zero;
+    uint2* dst = reinterpret_cast<uint2*>(codes + m * steps * 32);
+    for (int o = threadIdx.x; o < steps * 64; o += kFewThreads) {
       uint2 q = make_uint2(0, 0);
-      if (m < a.m && !rs.zero) {
-        const T* src = x + m * a.ldx + o * 8;
+      if (some && o * 8 < whole) {
         float v[8];
-        if (octets && o * 8 + 8 <= a.k) {
+        if (octets) {
           Octet<T> raw;
-          raw.load(src);
+          raw.load_shared(src + o * 8);
           raw.unpack(v);
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = o * 8 + j < a.k ? Storage<T>::load1(src + j) : 0.0f;
+          for (int j = 0; j < 8; ++j) v[j] = Storage<T>::load1(src + o * 8 + j);
         }
         q = make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
       }
       dst[o] = q;
     }
+    if (threadIdx.x < 16) rest[m][threadIdx.x] = static_cast<int8_t>(some && whole + threadIdx.x < a.k ? code_of(Storage<T>::load1(src + whole + threadIdx.x), rs.inv) : 0);
   }
   __syncthreads();
-  if (n0 >= a.n) return;
-  int acc[kFewChannels][M] = {};
-  for (int base = 0; base < chunks; base += 32 * kFewAhead) {
+  bool ok = true;
+  int slot = 0;
+  uint32_t parity = 0;
+  int sum[M] = {};                                      // lane i: of the i-th of 32 channels
+  for (int64_t i = 0; i < mine && ok; ++i) {
+    const int64_t n0 = first + i * stride;
+    int acc[M] = {};
+    for (int segment = 0; segment < segments; ++segment) {
+      ok = mbar_wait<false>(smem_u32(&full[warp][slot]), parity, aborted, &g_linear_error, 121);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const int count = (min(slot_bytes, whole - segment * slot_bytes) + 511) / 512;
+      const uint32_t from = own + slot * slot_bytes + lane * 16;
+      const uint4* t = codes + segment * (slot_bytes / 16) + lane;
+      // (behind the row's last code the slot holds old codes, and the tokens' are zero)
+      auto step = [&](int s) {
+        const uint4 w = lds128(from + s * 512);
 #pragma unroll
-    for (int i = 0; i < kFewAhead; ++i) {
-      const int ch = base + lane + 32 * i;
-      uint4 q[kFewChannels];
+        for (int m = 0; m < M; ++m) acc[m] = dot16(w, t[(m * steps + s) * 32], acc[m]);
+      };
+      if (count == kFewSegment / 512) {
 #pragma unroll
-      for (int c = 0; c < kFewChannels; ++c) q[c] = ahead[i][c];
-      const int next = ch + 32 * kFewAhead;
+        for (int s = 0; s < kFewSegment / 512; ++s) step(s);
+      } else {
+        for (int s = 0; s < count; ++s) step(s);
+      }
+      __syncwarp();
+      if (lane == 0 && issued < total) issue();
+      if (++slot == slots) slot = 0, parity ^= 1;
+    }
+    if (whole + lane < a.k) {                           // the end of the row, a code a lane: nothing behind the last one is read
+      const int w = a.w[n0 * a.ldw + whole + lane];
 #pragma unroll
-      for (int c = 0; c < kFewChannels; ++c) ahead[i][c] = next < whole ? load_codes16(w[c] + next * 16) : make_uint4(0, 0, 0, 0);
-      if (ch < chunks) {
-        if (ch >= whole) {                         // the end of the row: nothing behind its last code is read
+      for (int m = 0; m < M; ++m) acc[m] += w * rest[m][lane];
+    }
 #pragma unroll
-          for (int c = 0; c < kFewChannels; ++c) {
-            uint32_t word[4] = {0, 0, 0, 0};
-            for (int j = 0; ch * 16 + j < a.k; ++j) word[j >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(w[c][ch * 16 + j])) << (8 * (j & 3));
-            q[c] = make_uint4(word[0], word[1], word[2], word[3]);
-          }
-        }
+    for (int m = 0; m < M; ++m) {
+      const int all = __reduce_add_sync(0xFFFFFFFFu, acc[m]);
+      if (lane == static_cast<int>(i & 31)) sum[m] = all;
+    }
+    if ((i & 31) == 31 || i + 1 == mine) {
+      const int64_t n = first + ((i & ~int64_t{31}) + lane) * stride;
+      if (ok && lane <= static_cast<int>(i & 31)) {
+        const float sw = a.sw[n], bias = a.bias ? load_one<T>(a.bias, n) : 0.0f;
+        const bool drop = a.mask.threshold != 0;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-          const uint4 t = few_codes[m * chunks + ch];
-#pragma unroll
-          for (int c = 0; c < kFewChannels; ++c) acc[c][m] = dot16(q[c], t, acc[c][m]);
+          if (m < a.m) {
+            const bool keep = drop && (keep_bits(a.mask, static_cast<uint64_t>(m * ((a.n + 7) / 8) + (n >> 3))) >> (n & 7) & 1);
+            const float v = finish1(sum[m], sx[m], sw, bias, a.residual ? load_one<T>(a.residual, m * a.ldr + n) : 0.0f, keep, a.mask.scale, drop);
+            Storage<T>::store1(static_cast<T*>(a.y) + m * a.ldy + n, v);
+          }
         }
       }
     }
   }
-  int sum = 0;                                     // lane c * M + m: that of channel c and token m
-#pragma unroll
-  for (int c = 0; c < kFewChannels; ++c)
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      const int all = __reduce_add_sync(0xFFFFFFFFu, acc[c][m]);
-      if (lane == c * M + m) sum = all;
+  if (!ok && lane == 0)                                 // the copies in flight: those of the slots from here on
+    for (int i = 0; i < slots && i < issued; ++i) {
+      mbar_drain(smem_u32(&full[warp][slot]), parity);
+      if (++slot == slots) slot = 0, parity ^= 1;
     }
-  const int m = lane % M;
-  const int64_t n = n0 + lane / M;
-  if (lane < kFewChannels * M && n < a.n && m < a.m) {
-    const bool drop = a.mask.threshold != 0;
-    const bool keep = drop && (keep_bits(a.mask, static_cast<uint64_t>(m * ((a.n + 7) / 8) + (n >> 3))) >> (n & 7) & 1);
-    const float v = finish1(sum, sx[m], a.sw[n], a.bias ? load_one<T>(a.bias, n) : 0.0f, a.residual ? load_one<T>(a.residual, m * a.ldr + n) : 0.0f, keep,
-                            a.mask.scale, drop);
-    Storage<T>::store1(static_cast<T*>(a.y) + m * a.ldy + n, v);
-  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -367,6 +411,7 @@ struct TileShape {
   int32_t split;         // CTAs of a cluster that share a tile
   int32_t stages;
   int32_t token_tiles;
+  int32_t weights_ahead; // 1: the kernel in front is the tokens' quantiser, which lets this one start after its own wait: the weights are older
 };
 
 // kind::i8: signed 8-bit operands, both K-major, 32-bit integer accumulator, M = 128, N = n
@@ -412,14 +457,15 @@ __device__ __forceinline__ void residual_ahead(const LinearArgs& a, int64_t m0, 
 #pragma unroll
   for (int j = 0; j < U; ++j) add[j] = p[min(m0 + j, a.m - 1) * a.ldr];
 }
-// The scales of the tokens that a warp of the epilogue finishes (the batches of 16 that start at 16 `half`, 32 apart) into its own 128 places: no
+// The scales of the tokens that a warp of the epilogue finishes (the batches of 16 that start at 16 `part`, STEP apart) into places of its own: no
 // barrier between warps, so that a warp that gives up a wait leaves nobody behind.
-__device__ __forceinline__ void load_scales(const LinearArgs& a, int64_t m0, int half, int tokens, float* own) {
+template <int STEP>
+__device__ __forceinline__ void load_scales(const LinearArgs& a, int64_t m0, int part, int tokens, float* own) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = i * 32 + lane, c = (j & 15) + 16 * half + (j >> 4) * 32;
+  for (int i = 0; i < (256 + STEP - 1) / STEP / 2; ++i) {      // two batches a turn
+    const int j = i * 32 + lane, c = (j & 15) + 16 * part + (j >> 4) * STEP;
     if (c < tokens) own[j] = a.sx[min(m0 + c, a.m - 1)];
   }
   __syncwarp();
@@ -439,21 +485,17 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum
     const uint32_t bits = DROP ? __shfl_sync(0xFFFFFFFFu, keep[j / 8], (lane & 24) | (j & 7)) : 0u;
     v[j] = finish1(static_cast<int>(sum[j]), sx[j], sw, bias, a.residual ? Storage<T>::load1(add + j) : 0.0f, bits >> (lane & 7) & 1, a.mask.scale, DROP);
   }
-  T* y = static_cast<T*>(a.y) + m0 * a.ldy + n;
   if (n < a.n) {
+    T* y = static_cast<T*>(a.y) + m0 * a.ldy + n;
+    if (m0 + U <= a.m) {
 #pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (m0 + j < a.m) Storage<T>::store1(y + j * a.ldy, v[j]);
-  }
-}
-
-// Waits for the kernel in front: the tokens' codes and scales, the last users of y.
-__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-// What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too.
-__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
-  const unsigned long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+      for (int j = 0; j < U; ++j, y += a.ldy) Storage<T>::store1(y, v[j]);
+    } else {
+      const int left = static_cast<int>(a.m - m0);
+#pragma unroll
+      for (int j = 0; j < U; ++j, y += a.ldy)
+        if (j < left) Storage<T>::store1(y, v[j]);
+    }
   }
 }
 
@@ -496,9 +538,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   bool ok = true;
   if (warp == 0) {
     if (elect_one()) {
-      // The first stages' weights are fetched before the wait for the kernel in front, which is the tokens' quantiser or none: that kernel
-      // writes the workspace only, and it began when everything older was done.
-      const int ahead = min(shape.stages, last - first);
+      // behind the tokens' quantiser: the first stages' weights are fetched before the wait for it
+      const int ahead = shape.weights_ahead ? min(shape.stages, last - first) : 0;
       for (int s = 0; s < ahead; ++s) {
         mbar_arrive_expect_tx(smem_u32(&full[s]), stage_bytes);
         tma_load_2d(stages0 + s * stage_bytes, &map_w, (first + s) * kChunk, static_cast<int>(n0), smem_u32(&full[s]));
@@ -549,7 +590,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   float sw = 0.0f, bias = 0.0f;
   if (warp >= 2) {
     dependency_wait();
-    load_scales(a, m0, half, shape.tokens, scales[warp - 2]);
+    load_scales<32>(a, m0, half, shape.tokens, scales[warp - 2]);
     if (n < a.n) {
       sw = a.sw[n];
       if (a.bias) bias = load_one<T>(a.bias, n);
@@ -652,17 +693,21 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t ncols
   asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// Twelve epilogue warps: with eight, two a scheduler, their waits for tensor memory showed (333 x 1027 -> 50265 tokens in fp32), with sixteen
+// the registers do not reach.  An accumulator is given back as soon as its last columns are in registers, with a release within the CTA: one for the cluster
+// made the warp wait for its stores.
+constexpr int kPairEpilogue = 12, kPairThreads = 64 + kPairEpilogue * 32, kPairStep = kPairEpilogue / 4 * 16;
 template <typename T, bool DROP>
-__global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+__global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                                    const LinearArgs a, const TileShape shape, const int64_t tiles) {
   extern __shared__ uint8_t pair_smem[];
   __shared__ __align__(8) uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  __shared__ float scales[8][128];
+  __shared__ float scales[kPairEpilogue][96];
   const uint32_t stages0 = (smem_u32(pair_smem) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = blockIdx.x & 1;
@@ -678,7 +723,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&acc_full[i]), 1);
-      mbar_init(smem_u32(&acc_empty[i]), 16);
+      mbar_init(smem_u32(&acc_empty[i]), 2 * kPairEpilogue);
     }
     fence_mbar_init();
   }
@@ -696,7 +741,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
     if (elect_one()) {
       bool ok = true;
       // weights before the wait, as in linear_tile_kernel
-      const int ahead = min(kPairStages, chunks), stage_bytes = (kTileChannels + half_tokens) * kChunk;
+      const int ahead = shape.weights_ahead ? min(kPairStages, chunks) : 0, stage_bytes = (kTileChannels + half_tokens) * kChunk;
       for (int s = 0; s < ahead; ++s) {
         if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * stage_bytes);
         tma_load_pair(stages0 + s * kPairStageBytes, &map_w, s * kChunk, static_cast<int>(pair / shape.token_tiles * 256 + rank * 128), peer_smem(smem_u32(&full[s]), 0));
@@ -748,7 +793,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
     }
     __syncwarp();
   } else {
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const int quarter = warp & 3, part = (warp - 2) >> 2;   // three warps a quarter of the rows, batches of 16 tokens in turn
     const uint32_t mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     bool ok = true;
     int turn = 0;
@@ -756,30 +801,39 @@ __global__ void __launch_bounds__(kTileThreads) linear_pair_kernel(const __grid_
     for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
       const int acc = turn & 1;
       const int64_t n = t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, m0 = t % shape.token_tiles * shape.tokens;
-      load_scales(a, m0, half, shape.tokens, scales[warp - 2]);
+      load_scales<kPairStep>(a, m0, part, shape.tokens, scales[warp - 2]);
       const float sw = n < a.n ? a.sw[n] : 0.0f, bias = a.bias && n < a.n ? load_one<T>(a.bias, n) : 0.0f;
       T add[16];
-      if (a.residual) residual_ahead<T, 16>(a, m0 + half * 16, n, add);
+      if (a.residual) residual_ahead<T, 16>(a, m0 + part * 16, n, add);
       ok = mbar_wait<false>(smem_u32(&acc_full[acc]), turn >> 1 & 1, aborted, &g_linear_error, 114);
       ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
       ok = __all_sync(0xFFFFFFFFu, ok);
       tc_fence_after();
       if (ok) {
-        for (int c = half * 16; c < shape.tokens && m0 + c < a.m; c += 32) {
+        const int most = static_cast<int>(min(static_cast<int64_t>(shape.tokens), a.m - m0));
+        bool held = true;
+        for (int c = part * 16; c < most; c += kPairStep) {
           uint32_t v[16];
           T next[16];
           tmem_ld16(mine + acc * 256 + c, v);
-          if (a.residual && c + 32 < shape.tokens) residual_ahead<T, 16>(a, m0 + c + 32, n, next);
+          if (a.residual && c + kPairStep < most) residual_ahead<T, 16>(a, m0 + c + kPairStep, n, next);
           tmem_ld_wait();
-          finish<T, DROP, 16>(a, v, scales[warp - 2] + c / 32 * 16, m0 + c, n, sw, bias, add);
+          if (c + kPairStep >= most) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
+            held = false;
+          }
+          finish<T, DROP, 16>(a, v, scales[warp - 2] + c / kPairStep * 16, m0 + c, n, sw, bias, add);
           if (a.residual) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) add[j] = next[j];
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
+        if (held) {                                         // (a warp without tokens in this tile)
+          __syncwarp();
+          if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
+        }
       }
     }
   }
@@ -871,88 +925,67 @@ int tile_smem_bytes(const TileShape& s) {
 }
 
 template <typename T, bool DROP>
-cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmemAlone + 1024);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[2];
-  cfg.blockDim = dim3(kTileThreads);
-  cfg.gridDim = dim3(static_cast<unsigned>((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split));
-  cfg.dynamicSmemBytes = static_cast<size_t>(tile_smem_bytes(s));
-  cfg.stream = st;
-  cfg.attrs = attr;
-  if (s.split > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = static_cast<unsigned>(s.split);
-    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
-    ++cfg.numAttrs;
-  }
-  if (behind_quantiser) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, DROP>, mw, mx, a, s);
+  const int64_t ctas = (a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split;
+  return launch_behind(linear_tile_kernel<T, DROP>, static_cast<unsigned>(ctas), kTileThreads, tile_smem_bytes(s), s.split, st, mw, mx, a, s);
 }
-
 template <typename T, bool DROP>
-cudaError_t launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+cudaError_t launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
   constexpr int smem = kPairStages * kPairStageBytes + 1024;
   cudaError_t e = cudaFuncSetAttribute(linear_pair_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (a.n + 255) / 256 * s.token_tiles;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[2];
-  cfg.blockDim = dim3(kTileThreads);
-  cfg.gridDim = dim3(static_cast<unsigned>(2 * std::min<int64_t>(tiles, kPairs)));
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.numAttrs = 1;
-  if (behind_quantiser) {
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.numAttrs = 2;
-  }
-  return cudaLaunchKernelEx(&cfg, linear_pair_kernel<T, DROP>, mw, mx, a, s, tiles);
+  return launch_behind(linear_pair_kernel<T, DROP>, static_cast<unsigned>(2 * std::min<int64_t>(tiles, kPairs)), kPairThreads, smem, 2, st, mw, mx, a, s, tiles);
 }
 
 template <typename T>
-cudaError_t launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, bool behind_quantiser, cudaStream_t st) {
+cudaError_t launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
   const bool drop = a.mask.threshold != 0;
-  if (s.pair) return drop ? launch_pair<T, true>(mw, mx, a, s, behind_quantiser, st) : launch_pair<T, false>(mw, mx, a, s, behind_quantiser, st);
-  return drop ? launch_tile<T, true>(mw, mx, a, s, behind_quantiser, st) : launch_tile<T, false>(mw, mx, a, s, behind_quantiser, st);
+  if (s.pair) return drop ? launch_pair<T, true>(mw, mx, a, s, st) : launch_pair<T, false>(mw, mx, a, s, st);
+  return drop ? launch_tile<T, true>(mw, mx, a, s, st) : launch_tile<T, false>(mw, mx, a, s, st);
 }
 
 // Product of codes with the tensor cores.
 int run_product(const int8_t* xq, int64_t ldq, const LinearArgs& a, int32_t dtype, bool behind_quantiser, cudaStream_t st) {
-  const TileShape s = tile_shape(a.m, a.n, a.k);
+  TileShape s = tile_shape(a.m, a.n, a.k);
+  s.weights_ahead = behind_quantiser;
   if ((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split > 0x7FFFFFFF) return ZGR_ETOOBIG;
   CUtensorMap mw, mx;
   if (!codes_map(&mw, a.w, a.n, a.k, a.ldw, kTileChannels) || !codes_map(&mx, xq, a.m, a.k, ldq, s.pair ? s.tokens / 2 : s.tokens)) return ZGR_ECUDA;
-  const cudaError_t e = dtype == ZGR_F32   ? launch_product<float>(mw, mx, a, s, behind_quantiser, st)
-                        : dtype == ZGR_F16 ? launch_product<__half>(mw, mx, a, s, behind_quantiser, st)
-                                           : launch_product<__nv_bfloat16>(mw, mx, a, s, behind_quantiser, st);
+  const cudaError_t e = dtype == ZGR_F32   ? launch_product<float>(mw, mx, a, s, st)
+                        : dtype == ZGR_F16 ? launch_product<__half>(mw, mx, a, s, st)
+                                           : launch_product<__nv_bfloat16>(mw, mx, a, s, st);
   return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
+// The slots of a warp in the kernel for few tokens: rows, or equal parts of them up to 4096 bytes, eight if they fit, two at least; 0: the
+// tokens' rows leave no room.
+struct FewShape {
+  int slots, bytes;
+};
+FewShape few_shape(int64_t m, int64_t k) {
+  const int row = std::max(512, few_pitch(static_cast<int>(k))), parts = (row + kFewSegment - 1) / kFewSegment;
+  FewShape s = {0, few_pitch((row + parts - 1) / parts)};
+  if (m > kFewTokens) return s;
+  const int64_t left = (kFewSmem - m * few_pitch(static_cast<int>(k))) / (kFewWarps * s.bytes);
+  s.slots = left >= 2 ? static_cast<int>(std::min<int64_t>(left, kFewSlots)) : 0;
+  return s;
+}
+bool few(int64_t m, int64_t k) { return few_shape(m, k).slots > 0; }
 template <typename T, int M>
 cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
   if (e != cudaSuccess) return e;
-  const int64_t per_block = kFewThreads / 32 * kFewChannels;
-  linear_few_kernel<T, M><<<static_cast<unsigned>((a.n + per_block - 1) / per_block), kFewThreads, M * ((a.k + 15) / 16) * 16, st>>>(a);
-  return cudaGetLastError();
+  const FewShape s = few_shape(M, a.k);
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((a.n + 3) / 4, 148));      // (four warps of a block at least have something to do)
+  return launch_behind(linear_few_kernel<T, M>, blocks, kFewThreads, kFewWarps * s.slots * s.bytes + M * few_pitch(a.k), 1, st, a, s.slots, s.bytes);
 }
 template <typename T>
 cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
-  return a.m == 1 ? launch_few<T, 1>(a, st) : (a.m == 2 ? launch_few<T, 2>(a, st) : launch_few<T, kFewTokens>(a, st));
+  return a.m == 1 ? launch_few<T, 1>(a, st) : launch_few<T, kFewTokens>(a, st);
 }
-// Tokens that the kernel for few of them takes: what fits its shared memory, up to four.
-bool few(int64_t m, int64_t k) { return m <= kFewTokens && (m == 1 ? 1 : (m == 2 ? 2 : 4)) * ((k + 15) / 16 * 16) <= kFewSmem; }
 
 constexpr int64_t kMaxInner = 1 << 17;      // 127 * 127 * 2^17 < 2^31: the sums fit 32 bits
 
