@@ -137,7 +137,83 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
   }
 }
 
-// Rows that do not start on 16-byte boundaries (an odd number of columns), all matrices alike.  A row's pieces of eight elements then begin `s`
+// Rows that follow each other without a gap and are no whole octets (an odd number of columns, at least eight).  The tensor is cut in pieces of
+// eight elements wherever a row ends, so that all accesses are whole and aligned; a piece from column c on takes its bits from the block
+// of c, made here, from the next piece's, got from the next lane, and, where the row ends within it, sometimes from a third, made by that lane
+// alone.  fp16, 16336 x 1021: 27.8 us by the rows' own pieces (dropout_shifted_kernel), whose ends are loaded and stored element by element.
+template <typename T, int U>
+__global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid_constant__ DropArgs<T> a) {
+  const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
+  dependency_wait();
+  const int64_t elements = a.rows * a.cols;
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
+  Octet<T> x[U], r[U];
+  int64_t row[U];
+  int col[U];
+  uint32_t own[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = min(first + u * 32, a.total - 1), e = i * 8;
+    row[u] = elements < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(e), a.div)) : e / a.cols;
+    col[u] = static_cast<int>(e - row[u] * a.cols);
+    if (e + 8 <= elements) {
+      x[u].load(a.x + e);
+      if (a.residual) r[u].load(a.residual + e);
+    } else {                                                   // the end of the tensor
+      x[u].gather(a.x + e, 0, static_cast<int>(elements - e));
+      if (a.residual) r[u].gather(a.residual + e, 0, static_cast<int>(elements - e));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) own[u] = keep_bits(a.mask, static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3)));
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * 32;
+    // the next piece's block: of this row, or the first of the next
+    uint32_t next = __shfl_down_sync(0xFFFFFFFFu, own[u], 1);
+    if (u + 1 < U) {
+      const uint32_t over = __shfl_sync(0xFFFFFFFFu, own[u + 1 < U ? u + 1 : u], 0);
+      if (lane == 31) next = over;
+    }
+    const int s = col[u] & 7, left = cols - col[u];            // elements of the row from here on
+    const uint64_t block = static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3));
+    if (u + 1 == U && lane == 31) next = keep_bits(a.mask, left > 8 ? block + 1 : static_cast<uint64_t>((row[u] + 1) * a.octets));
+    uint32_t rest = next;                                      // behind this block in the same row
+    if (left <= 8 && left > 8 - s) rest = keep_bits(a.mask, block + 1);
+    uint32_t keep = own[u] >> s | rest << (8 - s);
+    if (left < 8) keep = (keep & ((1u << left) - 1)) | next << left;
+    if (i < a.total) {
+      float v[8];
+      x[u].unpack(v);
+      if (a.bias) {
+        T b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = a.bias[j < left ? col[u] + j : j - left];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += Storage<T>::load1(b + j);
+      }
+      if (a.residual) {
+        float add[8];
+        r[u].unpack(add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = masked_plus(v[j], keep >> j & 1, a.mask.scale, add[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = masked(v[j], keep >> j & 1, a.mask.scale);
+      }
+      T* y = a.y + i * 8;
+      if (i * 8 + 8 <= elements) {
+        Storage<T>::store8(y, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (i * 8 + j < elements) Storage<T>::store1(y + j, v[j]);
+      }
+    }
+  }
+}
+
+// Rows that do not start on 16-byte boundaries, all matrices alike.  A row's pieces of eight elements then begin `s`
 // elements before it, at the boundary, and take the last s bits of one generator block and the first 8 - s of the next: a thread
 // makes the block of its own piece and gets its neighbour's bits from the neighbouring lane; a warp's pieces follow each other, so that only its
 // first lane makes a second block, once for U pieces.
@@ -386,10 +462,17 @@ int run_dropout(DropArgs<T> a, cudaStream_t st) {
     a.div = make_fast_div(static_cast<uint32_t>(std::min<int64_t>(a.pieces, 0x7FFFFFFF)));
     a.bias_octets = aligned_to(a.bias, 16);
     const bool flat = !shift && plain;
+    // without a gap between the rows, but not whole octets
+    const bool unbroken = a.phase == 0 && a.cols >= 8 && a.cols % 8 != 0 && a.rows > 1 && a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols);
+    if (unbroken) {
+      a.total = (a.rows * a.cols + 7) / 8;
+      a.div = make_fast_div(static_cast<uint32_t>(a.cols));
+    }
     const bool small = a.total < int64_t{148} * 8 * kThreads;
     const int64_t per_block = kThreads * (small ? 1 : kMany), blocks = (a.total + per_block - 1) / per_block;
     if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-    const auto kernel = shift ? (small ? dropout_shifted_kernel<T, 1> : dropout_shifted_kernel<T, kMany>)
+    const auto kernel = unbroken ? (small ? dropout_unbroken_kernel<T, 1> : dropout_unbroken_kernel<T, kMany>)
+                        : shift ? (small ? dropout_shifted_kernel<T, 1> : dropout_shifted_kernel<T, kMany>)
                         : flat ? (small ? dropout_kernel<T, 1, true> : dropout_kernel<T, kMany, true>)
                                : (small ? dropout_kernel<T, 1, false> : dropout_kernel<T, kMany, false>);
     return launch_behind(kernel, static_cast<unsigned>(blocks), kThreads, 0, 1, st, a) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;

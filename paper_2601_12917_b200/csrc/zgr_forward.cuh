@@ -69,6 +69,35 @@ struct Octet {
 #pragma unroll
     for (int j = 0; j < 8; ++j) e[j] = row[max(0, min(c + j, cols - 1))];
   }
+  // Elements p[0 .. 7] at any alignment: the 16-byte granules that hold them (all of [lo, hi) that load_any_ok() asks for), moved into place
+  // by selections and one funnel shift a word.  About 20 instructions instead of eight loads.
+  __device__ __forceinline__ void load_any(const T* p) {
+    constexpr int kWords = 4 * sizeof(T) / 2;      // of an octet
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const uint4* base = reinterpret_cast<const uint4*>(at & ~uintptr_t{15});
+    uint32_t g[kWords + 4];
+#pragma unroll
+    for (int i = 0; i < kWords / 4 + 1; ++i) {
+      const uint4 q = __ldg(base + i);
+      g[4 * i] = q.x, g[4 * i + 1] = q.y, g[4 * i + 2] = q.z, g[4 * i + 3] = q.w;
+    }
+    const bool two = at & 8, one = at & 4, half = at & 2;
+#pragma unroll
+    for (int i = 0; i < kWords + 2; ++i) g[i] = two ? g[i + 2] : g[i];
+#pragma unroll
+    for (int i = 0; i < kWords + 1; ++i) g[i] = one ? g[i + 1] : g[i];
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) g[i] = half ? __funnelshift_r(g[i], g[i + 1], 16) : g[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) w[i] = make_uint4(g[4 * i], g[4 * i + 1], g[4 * i + 2], g[4 * i + 3]);
+  }
+  // Whether the granules of load_any(p) lie within the elements [lo, hi).
+  static __device__ __forceinline__ bool load_any_ok(const T* p, const T* lo, const T* hi) {
+    const uintptr_t base = reinterpret_cast<uintptr_t>(p) & ~uintptr_t{15};
+    return base >= reinterpret_cast<uintptr_t>(lo) && base + 16 * (sizeof(T) / 2 + 1) <= reinterpret_cast<uintptr_t>(hi);
+  }
   __device__ __forceinline__ void unpack(float (&v)[8]) const;
 };
 template <>

@@ -48,82 +48,73 @@ __device__ __forceinline__ uint32_t code4(const float* v, float inv) {
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// Threads per row: WARPS warps; a block has rows for at least four warps.  A thread holds NV octets (OCTETS: rows of both matrices on
-// 16-byte and 8-byte boundaries) or 8 NV single elements, so a row of up to WARPS * NV * 256 elements is read once.
+// A row is read once and stays in registers between the two passes over it, NV octets a thread, as few as hold it (idle lanes cost as much as
+// the others).  ROWS = 4: four warps a block with a row each, up to 1536 elements; ROWS = 1: a block a row, with four, eight or twelve
+// warps, at most six octets a thread.  4096 rows of 11008 bf16 elements: 27 us with eight warps and six octets, 34 with sixteen and three
+// or with eleven and four.
+// The rows of x may start anywhere (ALIGNED = false: octets are put together from 16-byte granules, one by one at the row's ends), as may
+// those of the codes (`wide` = 0: written byte by byte).
 // early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not.
-template <typename T, int WARPS, int NV, bool OCTETS>
-__global__ void __launch_bounds__(WARPS < 4 ? 128 : WARPS * 32) quantize_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t rows,
-                                                                                     const int cols, int8_t* __restrict__ codes, const int64_t ldc,
-                                                                                     float* __restrict__ scales, const int early) {
-  constexpr int kPerRow = WARPS * 32, kRows = WARPS < 4 ? 4 / WARPS : 1;
-  __shared__ uint32_t part[kRows][WARPS];
+template <typename T, int ROWS, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(ROWS == 4 ? 128 : 384) quantize_rows_kernel(const T* x, const int64_t ldx, const int64_t rows, const int cols, int8_t* codes,
+                                                                              const int64_t ldc, float* scales, const int wide, const int early) {
+  __shared__ uint32_t part[16];
   dependency_wait();
   if (early) dependents_may_start();
-  const int t = threadIdx.x % kPerRow, which = threadIdx.x / kPerRow;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + which;
-  const bool inside = row < rows;
-  const T* src = x + min(row, rows - 1) * ldx;
-  Octet<T> raw[OCTETS ? NV : 1];
-  T one[OCTETS ? 1 : 8 * NV];
+  const int threads = ROWS == 4 ? 32 : blockDim.x, t = ROWS == 4 ? threadIdx.x & 31 : threadIdx.x;
+  const int64_t row = ROWS == 4 ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5) : blockIdx.x;
+  if (ROWS == 4 && row >= rows) return;                        // (whole warps)
+  const T* src = x + row * ldx;
+  Octet<T> raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * threads) * 8;
+    raw[i].zero();
+    if (ALIGNED) {
+      if (c + 8 <= cols) raw[i].load(src + c);
+    } else if (c + 8 <= cols && Octet<T>::load_any_ok(src + c, src, src + cols)) {
+      raw[i].load_any(src + c);
+    } else if (c < cols) {
+      raw[i].gather(src, c, cols);                             // (behind the end: the row's last element again, which changes no maximum)
+    }
+  }
   uint32_t amax = 0;
-  if constexpr (OCTETS) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * kPerRow) * 8;
-      raw[i].zero();
-      if (inside && c + 8 <= cols) raw[i].load(src + c);
-    }
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * threads) * 8;
+    if (ALIGNED && c < cols && c + 8 > cols) raw[i].gather(src, c, cols);
+    float v[8];
+    raw[i].unpack(v);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * kPerRow) * 8;
-      float v[8];
-      raw[i].unpack(v);
-      if (inside && c < cols && c + 8 > cols)
-        for (int j = 0; c + j < cols; ++j) amax = max(amax, magnitude(Storage<T>::load1(src + c + j)));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = max(amax, magnitude(v[j]));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8 * NV; ++i) {
-      one[i] = src[min(t + i * kPerRow, cols - 1)];          // (clamped, not guarded: a guarded load is a branch, and they wait for each other)
-    }
-#pragma unroll
-    for (int i = 0; i < 8 * NV; ++i) amax = max(amax, magnitude(Storage<T>::load1(one + i)));
+    for (int j = 0; j < 8; ++j) amax = max(amax, magnitude(v[j]));
   }
   amax = __reduce_max_sync(0xFFFFFFFFu, amax);
-  if (WARPS > 1) {
-    if ((threadIdx.x & 31) == 0) part[which][t >> 5] = amax;
+  if (ROWS == 1) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = amax;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) amax = max(amax, part[which][w]);
+    for (int w = 0; w < threads / 32; ++w) amax = max(amax, part[w]);
   }
-  if (!inside) return;
   const RowScale rs = row_scale(amax);
   if (t == 0) scales[row] = rs.scale;
   int8_t* dst = codes + row * ldc;
-  if constexpr (OCTETS) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * kPerRow) * 8;
-      if (c + 8 <= cols) {
-        float v[8];
-        raw[i].unpack(v);
-        *reinterpret_cast<uint2*>(dst + c) = rs.zero ? make_uint2(0, 0) : make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
-      } else {
-        for (int j = 0; c + j < cols; ++j) dst[c + j] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(src + c + j), rs.inv));
-      }
-    }
-  } else {
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * threads) * 8;
+    float v[8];
+    raw[i].unpack(v);
+    const uint2 q = rs.zero ? make_uint2(0, 0) : make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
+    if (wide && c + 8 <= cols) {
+      *reinterpret_cast<uint2*>(dst + c) = q;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8 * NV; ++i) {
-      const int c = t + i * kPerRow;
-      if (c < cols) dst[c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(one + i), rs.inv));
+      for (int j = 0; j < 8; ++j)
+        if (c + j < cols) dst[c + j] = static_cast<int8_t>((j < 4 ? q.x : q.y) >> (8 * (j & 3)));
     }
   }
 }
 
-// Rows of more than 16384 elements: read twice, a block a row.
+// Rows of more than 18432 elements: read twice, a block a row.
+constexpr int64_t kLongRow = 18432;
 template <typename T>
 __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t cols, int8_t* __restrict__ codes,
                                                                  const int64_t ldc, float* __restrict__ scales, const int early) {
@@ -146,25 +137,28 @@ __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __rest
   for (int64_t c = threadIdx.x; c < cols; c += 512) codes[row * ldc + c] = static_cast<int8_t>(rs.zero ? 0 : code_of(Storage<T>::load1(src + c), rs.inv));
 }
 
-template <typename T, int WARPS, int NV>
+template <typename T, int ROWS, int NV>
 cudaError_t launch_rows(const T* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
-  const int per_block = WARPS < 4 ? 4 / WARPS : 1;
-  const unsigned grid = static_cast<unsigned>((rows + per_block - 1) / per_block);
-  const bool octets = octets_aligned(x, rows, ldx, sizeof(T)) && aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0);
-  return launch_behind(octets ? quantize_rows_kernel<T, WARPS, NV, true> : quantize_rows_kernel<T, WARPS, NV, false>, grid, WARPS < 4 ? 128 : WARPS * 32, 0, 1, st, x, ldx,
-                       rows, static_cast<int>(cols), codes, ldc, scales, early);
+  const unsigned grid = static_cast<unsigned>((rows + ROWS - 1) / ROWS);
+  const int threads = ROWS == 4 ? 128 : static_cast<int>((cols + 6143) / 6144) * 128;
+  const int wide = aligned_to(codes, 8) && (rows <= 1 || ldc % 8 == 0);
+  const auto kernel = octets_aligned(x, rows, ldx, sizeof(T)) ? quantize_rows_kernel<T, ROWS, NV, true> : quantize_rows_kernel<T, ROWS, NV, false>;
+  return launch_behind(kernel, grid, threads, 0, 1, st, x, ldx, rows, static_cast<int>(cols), codes, ldc, scales, wide, early);
 }
 
 template <typename T>
 cudaError_t run_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early, cudaStream_t st) {
   const T* p = static_cast<const T*>(x);
-  if (cols <= 256) return launch_rows<T, 1, 1>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 512) return launch_rows<T, 1, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 1024) return launch_rows<T, 1, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 2048) return launch_rows<T, 4, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 4096) return launch_rows<T, 4, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 8192) return launch_rows<T, 16, 2>(p, ldx, rows, cols, codes, ldc, scales, early, st);
-  if (cols <= 16384) return launch_rows<T, 16, 4>(p, ldx, rows, cols, codes, ldc, scales, early, st);
+  if (cols <= 1536) {
+    constexpr decltype(&launch_rows<T, 4, 1>) by_octets[] = {launch_rows<T, 4, 1>, launch_rows<T, 4, 2>, launch_rows<T, 4, 3>,
+                                                             launch_rows<T, 4, 4>, launch_rows<T, 4, 5>, launch_rows<T, 4, 6>};
+    return by_octets[(cols + 255) / 256 - 1](p, ldx, rows, cols, codes, ldc, scales, early, st);
+  }
+  if (cols <= kLongRow) {
+    constexpr decltype(&launch_rows<T, 1, 2>) by_octets[] = {launch_rows<T, 1, 2>, launch_rows<T, 1, 3>, launch_rows<T, 1, 4>, launch_rows<T, 1, 5>, launch_rows<T, 1, 6>};
+    const int64_t a_turn = (cols + 6143) / 6144 * 1024;      // elements that the block's threads hold an octet each of
+    return by_octets[(cols + a_turn - 1) / a_turn - 2](p, ldx, rows, cols, codes, ldc, scales, early, st);
+  }
   return launch_behind(quantize_long_rows_kernel<T>, static_cast<unsigned>(rows), 512, 0, 1, st, p, ldx, cols, codes, ldc, scales, early);
 }
 cudaError_t run_quantize(int32_t dtype, const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* codes, int64_t ldc, float* scales, int early,
@@ -798,11 +792,31 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
     bool ok = true;
     int turn = 0;
     dependency_wait();
+    // what a tile's epilogue reads beside the sums is loaded during the tile before
+    float sx_ahead[3], sw_ahead = 0.0f;
+    T bias_ahead = {};
+    auto ahead = [&](int64_t t) {
+      const int64_t n = min(t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, a.n - 1), m0 = t % shape.token_tiles * shape.tokens;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int j = i * 32 + lane;                        // places of the batches of 16 that start at 16 `part`, kPairStep apart
+        sx_ahead[i] = a.sx[min(m0 + (j & 15) + 16 * part + (j >> 4) * kPairStep, a.m - 1)];
+      }
+      sw_ahead = a.sw[n];
+      if (a.bias) bias_ahead = static_cast<const T*>(a.bias)[n];
+    };
+    if (pair < tiles) ahead(pair);
     for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
       const int acc = turn & 1;
       const int64_t n = t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, m0 = t % shape.token_tiles * shape.tokens;
-      load_scales<kPairStep>(a, m0, part, shape.tokens, scales[warp - 2]);
-      const float sw = n < a.n ? a.sw[n] : 0.0f, bias = a.bias && n < a.n ? load_one<T>(a.bias, n) : 0.0f;
+      const int most = static_cast<int>(min(static_cast<int64_t>(shape.tokens), a.m - m0));
+      float* sx = scales[warp - 2];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 3; ++i) sx[i * 32 + lane] = sx_ahead[i];
+      __syncwarp();
+      const float sw = sw_ahead, bias = a.bias ? Storage<T>::load1(&bias_ahead) : 0.0f;
+      if (t + pairs < tiles) ahead(t + pairs);
       T add[16];
       if (a.residual) residual_ahead<T, 16>(a, m0 + part * 16, n, add);
       ok = mbar_wait<false>(smem_u32(&acc_full[acc]), turn >> 1 & 1, aborted, &g_linear_error, 114);
@@ -810,27 +824,32 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
       ok = __all_sync(0xFFFFFFFFu, ok);
       tc_fence_after();
       if (ok) {
-        const int most = static_cast<int>(min(static_cast<int64_t>(shape.tokens), a.m - m0));
-        bool held = true;
-        for (int c = part * 16; c < most; c += kPairStep) {
-          uint32_t v[16];
+        const uint32_t sums = mine + acc * 256;
+        uint32_t v[16];
+        int c = part * 16;
+        if (c < most) tmem_ld16(sums + c, v);
+        tmem_ld_wait();
+        for (; c < most; c += kPairStep) {
+          uint32_t w[16];
           T next[16];
-          tmem_ld16(mine + acc * 256 + c, v);
-          if (a.residual && c + kPairStep < most) residual_ahead<T, 16>(a, m0 + c + kPairStep, n, next);
-          tmem_ld_wait();
-          if (c + kPairStep >= most) {
+          const bool more = c + kPairStep < most;
+          if (more) {
+            tmem_ld16(sums + c + kPairStep, w);
+            if (a.residual) residual_ahead<T, 16>(a, m0 + c + kPairStep, n, next);
+          }
+          if (!more) {                                      // all of this warp's columns are in registers
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
-            held = false;
           }
-          finish<T, DROP, 16>(a, v, scales[warp - 2] + c / kPairStep * 16, m0 + c, n, sw, bias, add);
-          if (a.residual) {
+          finish<T, DROP, 16>(a, v, sx + c / kPairStep * 16, m0 + c, n, sw, bias, add);
+          if (more) {
+            tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) add[j] = next[j];
+            for (int j = 0; j < 16; ++j) v[j] = w[j], add[j] = next[j];
           }
         }
-        if (held) {                                         // (a warp without tokens in this tile)
+        if (part * 16 >= most) {                            // (a warp without tokens in this tile)
           __syncwarp();
           if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
         }

@@ -21,9 +21,9 @@ def codes_of(t):
     return t.cpu().numpy().astype(np.int64)
 
 
-# threads per row: one warp up to 1024 elements, four up to 4096, eight to 8192, sixteen to 16384, then the form that reads twice
+# one warp a row up to 1536 elements, four up to 6144, eight up to 12288, twelve up to 18432, then the form that reads twice; octets a thread
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 7), (9, 8), (3, 33), (130, 64), (7, 1000), (2, 1024), (3, 1025), (5, 4096), (2, 4099), (3, 8192), (2, 11008), (2, 16384), (2, 16385), (1, 50265)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 7), (9, 8), (3, 33), (130, 64), (7, 1000), (2, 1024), (3, 1025), (4, 1536), (5, 1537), (3, 2049), (5, 4096), (2, 4099), (3, 6144), (2, 6145), (3, 8192), (2, 11008), (2, 12289), (2, 16384), (2, 18432), (2, 18433), (1, 50265)])
 def test_quantize_rows(rows, cols, dtype):
     x = make((rows, cols), dtype)
     if rows > 2:
