@@ -373,9 +373,9 @@ int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, v
                          uint64_t seed, uint32_t tensor, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Rows to signed 8-bit codes with a scale each, x ~ scale * code (the symmetric form of Sec. 3.4, zero point 0; what
- * zgr_set_coeffs_dtc reads with ldc = cols).  Per row, with a = max |x|:  scale = a / 127, code = rint(x * (127 / a)), where the quotients and
- * the product are fp32 numbers and rint takes ties to even: codes lie in [-127, 127], and each is within half a step of
- * x / scale, up to the rounding of the product (2^-16 of a step).  A row with a < 2^-120 gets codes 0 and scale 0, a row that holds an
+ * zgr_set_coeffs_dtc reads with ldc = cols).  Per row, with a = max |x|:  scale = a (1/127), code = rint(x (127 (1/a))), where both reciprocals
+ * and every product are rounded to fp32 and rint takes ties to even: codes lie in [-127, 127], and each is within half a step of
+ * x / scale, up to the rounding of the products (2^-14 of a step).  A row with a < 2^-120 gets codes 0 and scale 0, a row that holds an
  * infinity or a NaN codes 0 and scale NaN.  codes: rows x cols int8, ldc >= cols (nothing between the rows is written).  scales: rows fp32.
  * ZGR_EINVAL: null or misaligned pointer, cols < 1, rows < 0 or above 2^31 - 1, ld below cols, unknown dtype. */
 int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, int8_t* codes, int64_t ldc, float* scales, void* stream);

@@ -1,6 +1,6 @@
 // The linear layer of the forward pass in 8 bits: rows quantised with a scale each, the matrix product of two such matrices, and its epilogue.
 //
-//   quantise   a = max_k |x_k|,  scale = a / 127,  code_k = rint(x_k * (127 / a))         per row (a token, or a channel's weights)
+//   quantise   a = max_k |x_k|,  scale = a (1/127),  code_k = rint(x_k (127 (1/a)))        per row (a token, or a channel's weights)
 //   product    y[m][n] = residual[m][n] + D( (sum_k qx[m][k] qw[n][k]) * (sx[m] sw[n]) + bias[n] ),   D: dropout, or nothing
 //
 // The sums are 32-bit integers and exact; everything behind them is fp32, rounded once to the storage type.
@@ -22,7 +22,7 @@ __device__ int g_linear_error = 0;
 // ---------------------------------------------------------------------------------------------
 // Rows to codes.  Bound by memory: the row is read once and stays in registers between the two passes over it.
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kTinyBits = 0x03800000u;      // 2^-120: a row whose largest magnitude is below it counts as zero (127 / a stays finite)
+constexpr uint32_t kTinyBits = 0x03800000u;      // 2^-120: a row whose largest magnitude is below it counts as zero (127 (1/a) stays finite)
 constexpr uint32_t kInfBits = 0x7F800000u;
 
 struct RowScale {
@@ -34,12 +34,12 @@ __device__ __forceinline__ RowScale row_scale(uint32_t amax_bits) {
   RowScale r;
   const float a = __uint_as_float(amax_bits);
   r.zero = amax_bits < kTinyBits || amax_bits >= kInfBits;
-  r.inv = r.zero ? 0.0f : __fdiv_rn(127.0f, a);
-  r.scale = amax_bits < kTinyBits ? 0.0f : (amax_bits >= kInfBits ? __uint_as_float(0x7FC00000u) : __fdiv_rn(a, 127.0f));
+  r.inv = r.zero ? 0.0f : __fmul_rn(__frcp_rn(a), 127.0f);
+  r.scale = amax_bits < kTinyBits ? 0.0f : (amax_bits >= kInfBits ? __uint_as_float(0x7FC00000u) : __fmul_rn(a, 1.0f / 127.0f));
   return r;
 }
 // rint(fl(x inv)) in the low byte: adding 1.5 * 2^23 leaves the nearest integer (ties to even) in the low bits.  The product and the sum
-// are two roundings by definition (not a fused multiply-add).  |x inv| <= 127 (1 + 2^-23), so that no code is above 127.
+// are two roundings by definition (not a fused multiply-add).  |x inv| <= 127 (1 + 2^-20), so that no code is above 127.
 __device__ __forceinline__ uint32_t code_of(float x, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12582912.0f)) & 0xFFu; }
 __device__ __forceinline__ uint32_t code4(const float* v, float inv) {
   const uint32_t a = __float_as_uint(__fadd_rn(__fmul_rn(v[0], inv), 12582912.0f)), b = __float_as_uint(__fadd_rn(__fmul_rn(v[1], inv), 12582912.0f));

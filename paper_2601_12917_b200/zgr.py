@@ -8,7 +8,7 @@ missing the import of the library fails loudly -- there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
-import functools
+import importlib.util
 import os
 from typing import List, Optional, Sequence
 
@@ -148,209 +148,89 @@ def _stream_ptr(stream) -> Optional[int]:
 
 
 # -- operators of the forward pass --------------------------------------------------------------------------------
-# These calls last a few microseconds on the device, so their marshalling is kept short: attributes of a tensor are asked for once,
-# and strides only where a tensor is not contiguous.
+# Their marshalling is a compiled module (csrc/zgr_bind.cpp), built beside the library: they last a few microseconds on the device, and
+# ctypes with the checks around it took as long.  It calls the functions of the library loaded above.
 _STORAGE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
-_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_bind = None
 
 
-def _empty(shape, dtype, device, stream):
-    """An output or a workspace: it belongs to the stream that the work runs on (torch gives memory back to the stream it was made on)."""
-    if stream is None:
-        return torch.empty(*shape, dtype=dtype, device=device)
+def _load_bind():
+    global _bind
+    L = lib()
+    path = os.path.join(_HERE, "_zgr_bind.so")
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is missing: build it with `python -m paper_2601_12917_b200.build`")
+    spec = importlib.util.spec_from_file_location("_zgr_bind", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.zgr_dropout, L.zgr_dropout_backward, L.zgr_dropout_backward_workspace, L.zgr_quantize_rows,
+                                                                  L.zgr_linear_i8, L.zgr_linear_i8_workspace, L.zgr_matmul_i8)))
+    _bind = module
+    return module
+
+
+def _on_stream(f, stream, *args):
+    """The call on another stream than the current one: outputs and workspaces then belong to that stream, as torch keeps account of them."""
+    if stream.device.index != torch._C._cuda_getDevice():
+        raise ValueError("stream must be one of the current CUDA device")
     with torch.cuda.stream(stream):
-        return torch.empty(*shape, dtype=dtype, device=device)
-
-
-def _like(t, stream):
-    if stream is None and t.is_contiguous():
-        return torch.empty_like(t)
-    return _empty(t.shape, t.dtype, t.device, stream)
-
-
-def _pitch(t, what: str):
-    """(rows, columns, leading dimension) of a tensor whose last dimension is contiguous, its other dimensions as rows."""
-    shape = t.shape
-    if len(shape) == 2 and t.is_contiguous():
-        return shape[0], shape[1], shape[1]
-    if len(shape) == 0:
-        raise ValueError(f"{what} has no dimension")
-    if len(shape) != 2:
-        try:
-            t = t.view(t.numel() // shape[-1] if shape[-1] else 0, shape[-1])
-        except RuntimeError:
-            raise ValueError(f"{what}: the dimensions in front of the last are not one run of rows") from None
-    (rows, cols), (ld, step) = t.shape, t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"{what}: the last dimension must be contiguous")
-    return rows, cols, ld
-
-
-def _storage(t, what: str, dev: int) -> int:
-    if t.get_device() != dev:                # -1: not a CUDA tensor
-        raise ValueError(f"{what} must be on the current CUDA device")
-    code = _STORAGE.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{what} must be float32, float16 or bfloat16, not {t.dtype}")
-    return code
-
-
-def _same(t, what: str, dev: int, dtype, shape) -> int:
-    """Leading dimension of a tensor that has to be of this type and shape."""
-    if t.get_device() != dev:
-        raise ValueError(f"{what} must be on the current CUDA device")
-    if t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of shape {tuple(t.shape)}")
-    return shape[-1] if t.is_contiguous() else _pitch(t, what)[2]
-
-
-def _vector(t, what: str, dev: int, n: int, dtype) -> int:
-    if t is None:
-        raise ValueError(f"{what} is missing")
-    if t.get_device() != dev:
-        raise ValueError(f"{what} must be on the current CUDA device")
-    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous vector of {n} {dtype}")
-    return t.data_ptr()
-
-
-def _codes(t, what: str, dev: int):
-    if t.get_device() != dev:
-        raise ValueError(f"{what} must be on the current CUDA device")
-    if t.dtype != torch.int8 or t.dim() != 2:
-        raise ValueError(f"{what} must be a matrix of int8 codes")
-    return _pitch(t, what)
+        return f(*args)
 
 
 def dropout(x, p: float, seed: int, tensor: int = 0, bias=None, residual=None, out=None, stream=None):
     """residual + dropout(x + bias) with the mask of (seed, tensor), which is never stored (zgr_dropout).  x: (..., cols), its last
     dimension contiguous; residual and out: of the same shape; out may be x or residual itself.  Returns out."""
-    L, dev = _lib or lib(), _device()
-    code = _storage(x, "x", dev)
-    rows, cols, ldx = _pitch(x, "x")
-    pb = None if bias is None else _vector(bias, "bias", dev, cols, x.dtype)
-    pr, ldr = (None, 0) if residual is None else (residual.data_ptr(), _same(residual, "residual", dev, x.dtype, x.shape))
-    if out is None:
-        out, ldy = _like(x, stream), cols
-    else:
-        ldy = _same(out, "out", dev, x.dtype, x.shape)
-    rc = L.zgr_dropout(x.data_ptr(), ldx, pb, pr, ldr, out.data_ptr(), ldy, rows, cols, code, p, seed, tensor,
-                       _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if rc:
-        raise ZgrError(rc, "zgr_dropout")
-    return out
+    f = (_bind or _load_bind()).dropout
+    r = f(x, p, seed, tensor, bias, residual, out) if stream is None else _on_stream(f, stream, x, p, seed, tensor, bias, residual, out)
+    if r.__class__ is int:
+        raise ZgrError(r, "zgr_dropout")
+    return r
 
 
 def dropout_backward(dy, p: float, seed: int, tensor: int = 0, bias_grad: bool = False, out=None, stream=None):
     """Gradient of `dropout` with respect to x under the same (p, seed, tensor) (zgr_dropout_backward); with bias_grad a pair of it and
     the bias's gradient.  The residual's gradient is dy.  out may be dy itself."""
-    L, dev = _lib or lib(), _device()
-    code = _storage(dy, "dy", dev)
-    rows, cols, ldd = _pitch(dy, "dy")
-    if out is None:
-        out, ldx = _like(dy, stream), cols
-    else:
-        ldx = _same(out, "out", dev, dy.dtype, dy.shape)
-    db = pdb = pws = None
-    ws_bytes = 0
-    if bias_grad:
-        db = _empty((cols,), dy.dtype, dy.device, stream)
-        ws_bytes = _backward_workspace(rows, cols)
-        ws = _empty((ws_bytes,), torch.uint8, dy.device, stream)
-        pdb, pws = db.data_ptr(), ws.data_ptr()
-    rc = L.zgr_dropout_backward(dy.data_ptr(), ldd, out.data_ptr(), ldx, pdb, rows, cols, code, p, seed, tensor, pws, ws_bytes,
-                                _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if rc:
-        raise ZgrError(rc, "zgr_dropout_backward")
-    return (out, db) if bias_grad else out
-
-
-@functools.lru_cache(maxsize=4096)
-def _backward_workspace(rows: int, cols: int) -> int:
-    return lib().zgr_dropout_backward_workspace(rows, cols)
-
-
-@functools.lru_cache(maxsize=4096)
-def _linear_workspace(m: int, k: int) -> int:
-    return max(0, lib().zgr_linear_i8_workspace(m, k))      # (a size that is refused is refused by the call itself)
+    f = (_bind or _load_bind()).dropout_backward
+    r = f(dy, p, seed, tensor, bias_grad, out) if stream is None else _on_stream(f, stream, dy, p, seed, tensor, bias_grad, out)
+    if r.__class__ is int:
+        raise ZgrError(r, "zgr_dropout_backward")
+    return r
 
 
 def quantize_rows(x, pitch: Optional[int] = None, stream=None):
     """Signed 8-bit codes of the rows of x (rows, cols) with a scale each (zgr_quantize_rows).  Returns (codes, scales); rows of codes
     are `pitch` bytes apart, by default the next multiple of 16, which the products want; pitch = cols gives contiguous codes, which
     set_coeffs_dtc wants."""
-    L, dev = _lib or lib(), _device()
-    code = _storage(x, "x", dev)
-    if x.dim() != 2:
-        raise ValueError("x must be a matrix")
-    rows, cols, ldx = _pitch(x, "x")
-    if pitch is None:
-        pitch = (cols + 15) // 16 * 16
-    elif pitch < cols:
-        raise ValueError("pitch must not be below the number of columns")
-    device = x.device
-    codes, scales = _empty((rows, pitch), torch.int8, device, stream), _empty((rows,), torch.float32, device, stream)
-    rc = L.zgr_quantize_rows(x.data_ptr(), ldx, rows, cols, code, codes.data_ptr(), pitch, scales.data_ptr(),
-                             _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if rc:
-        raise ZgrError(rc, "zgr_quantize_rows")
-    return codes if pitch == cols else codes[:, :cols], scales
+    f = (_bind or _load_bind()).quantize_rows
+    r = f(x, pitch) if stream is None else _on_stream(f, stream, x, pitch)
+    if r.__class__ is int:
+        raise ZgrError(r, "zgr_quantize_rows")
+    return r
 
 
 def linear_i8(x, w, w_scale, bias=None, residual=None, p: float = 0.0, seed: int = 0, tensor: int = 0, out=None, stream=None):
     """residual + dropout(x w^T + bias) in 8 bits (zgr_linear_i8): x (..., k) is quantised with a scale for each token, w (n, k) and
     w_scale (n) are the codes and scales that quantize_rows makes of the weights.  Returns (..., n) of x's type."""
-    L, dev = _lib or lib(), _device()
-    code = _storage(x, "x", dev)
-    m, k, ldx = _pitch(x, "x")
-    n, kw, ldw = _codes(w, "w", dev)
-    if kw != k:
-        raise ValueError(f"w must have rows of {k} codes, not {kw}")
-    dtype, device = x.dtype, x.device
-    shape = (m, n) if x.dim() == 2 else (*x.shape[:-1], n)
-    ps = _vector(w_scale, "w_scale", dev, n, torch.float32)
-    pb = None if bias is None else _vector(bias, "bias", dev, n, dtype)
-    pr, ldr = (None, 0) if residual is None else (residual.data_ptr(), _same(residual, "residual", dev, dtype, shape))
-    if out is None:
-        out, ldy = _empty(shape, dtype, device, stream), n
-    else:
-        ldy = _same(out, "out", dev, dtype, shape)
-    ws_bytes = _linear_workspace(m, k)
-    pws = None
-    if ws_bytes:
-        ws = _empty((ws_bytes,), torch.uint8, device, stream)
-        pws = ws.data_ptr()
-    rc = L.zgr_linear_i8(x.data_ptr(), ldx, w.data_ptr(), ldw, ps, pb, pr, ldr, out.data_ptr(), ldy, m, n, k, code, p, seed, tensor, pws, ws_bytes,
-                         _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if rc:
-        raise ZgrError(rc, "zgr_linear_i8")
-    return out
+    f = (_bind or _load_bind()).linear_i8
+    r = (f(x, w, w_scale, bias, residual, p, seed, tensor, out) if stream is None
+         else _on_stream(f, stream, x, w, w_scale, bias, residual, p, seed, tensor, out))
+    if r.__class__ is int:
+        raise ZgrError(r, "zgr_linear_i8")
+    return r
 
 
 def matmul_i8(x, x_scale, w, w_scale, dtype=torch.bfloat16, bias=None, residual=None, p: float = 0.0, seed: int = 0, tensor: int = 0, out=None, stream=None):
     """linear_i8 for tokens that quantize_rows has made codes of already (zgr_matmul_i8): x (m, k), x_scale (m).  `dtype` is the type of
     the result, the bias and the residual."""
-    L, dev = _lib or lib(), _device()
-    if dtype not in _STORAGE:
+    f = (_bind or _load_bind()).matmul_i8
+    code = _STORAGE.get(dtype)
+    if code is None:
         raise ValueError("dtype must be float32, float16 or bfloat16")
-    m, k, ldx = _codes(x, "x", dev)
-    n, kw, ldw = _codes(w, "w", dev)
-    if kw != k:
-        raise ValueError(f"w must have rows of {k} codes, not {kw}")
-    pxs = _vector(x_scale, "x_scale", dev, m, torch.float32)
-    ps = _vector(w_scale, "w_scale", dev, n, torch.float32)
-    pb = None if bias is None else _vector(bias, "bias", dev, n, dtype)
-    pr, ldr = (None, 0) if residual is None else (residual.data_ptr(), _same(residual, "residual", dev, dtype, (m, n)))
-    if out is None:
-        out, ldy = _empty((m, n), dtype, x.device, stream), n
-    else:
-        ldy = _same(out, "out", dev, dtype, (m, n))
-    rc = L.zgr_matmul_i8(x.data_ptr(), ldx, pxs, w.data_ptr(), ldw, ps, pb, pr, ldr, out.data_ptr(), ldy, m, n, k, _STORAGE[dtype], p, seed, tensor,
-                         _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if rc:
-        raise ZgrError(rc, "zgr_matmul_i8")
-    return out
+    r = (f(x, x_scale, code, w, w_scale, bias, residual, p, seed, tensor, out) if stream is None
+         else _on_stream(f, stream, x, x_scale, code, w, w_scale, bias, residual, p, seed, tensor, out))
+    if r.__class__ is int:
+        raise ZgrError(r, "zgr_matmul_i8")
+    return r
 
 
 def linear_status() -> int:

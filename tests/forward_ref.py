@@ -47,15 +47,15 @@ def dropout(x, p, seed, tensor, bias=None, residual=None):
 
 
 def quantize(x):
-    """Codes (int64) and scales (float32), with the fp32 quotients and product that the definition names."""
+    """Codes (int64) and scales (float32), with the fp32 reciprocals and products that the definition names."""
     x = np.asarray(x, dtype=np.float32)
     with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
         a = np.abs(x).max(axis=1)
         bad = ~np.isfinite(x).all(axis=1)
         tiny = ~bad & (a < np.float32(2.0 ** -120))
-        inv = np.where(bad | tiny, np.float32(0), np.float32(127) / np.where(tiny, np.float32(1), a)).astype(np.float32)
+        inv = np.where(bad | tiny, np.float32(0), (np.float32(1) / np.where(tiny, np.float32(1), a)).astype(np.float32) * np.float32(127)).astype(np.float32)
         codes = np.rint(np.where(bad[:, None], np.float32(0), x) * inv[:, None]).astype(np.int64)
-        scale = np.where(tiny, np.float32(0), a / np.float32(127)).astype(np.float32)
+        scale = np.where(tiny, np.float32(0), a * (np.float32(1) / np.float32(127))).astype(np.float32)
     scale[bad] = np.nan
     return codes, scale
 
