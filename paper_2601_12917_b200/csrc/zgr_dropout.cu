@@ -166,6 +166,11 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) own[u] = keep_bits(a.mask, static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3)));
+  // the block behind a warp's pieces is the next warp's first; only behind the last warp's it is made once more
+  __shared__ uint32_t firsts[kThreads / 32];
+  const int warp = threadIdx.x >> 5;
+  if (lane == 0) firsts[warp] = own[0];
+  __syncthreads();
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = first + u * 32;
@@ -177,7 +182,14 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
     }
     const int s = col[u] & 7, left = cols - col[u];            // elements of the row from here on
     const uint64_t block = static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3));
-    if (u + 1 == U && lane == 31) next = keep_bits(a.mask, left > 8 ? block + 1 : static_cast<uint64_t>((row[u] + 1) * a.octets));
+    if (u + 1 == U) {
+      if (warp + 1 < kThreads / 32) {
+        const uint32_t over = firsts[warp + 1];
+        if (lane == 31) next = over;
+      } else if (lane == 31) {
+        next = keep_bits(a.mask, left > 8 ? block + 1 : static_cast<uint64_t>((row[u] + 1) * a.octets));
+      }
+    }
     uint32_t rest = next;                                      // behind this block in the same row
     if (left <= 8 && left > 8 - s) rest = keep_bits(a.mask, block + 1);
     uint32_t keep = own[u] >> s | rest << (8 - s);
@@ -320,10 +332,11 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
 // The backward pass with the bias's gradient: a block has a strip of 8 G columns and a range of rows, every thread eight fixed columns
 // (an octet, or the elements l, l + G, ... where rows start anywhere) whose sums it keeps in fp32.  The sums of a block meet in shared
 // memory, those of the ranges in the workspace, and column_sums_kernel adds them in a fixed order: the same bits every time.
-constexpr int kRowsInFlight = 4;
+// Four blocks on a multiprocessor, for which the grid is cut (cut_ranges): with 80 registers it was three, and a third of a second round.
 template <typename T, bool OCTETS>
-__global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials) {
+__global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials) {
   __shared__ float sums[kThreads * 8];
+  constexpr int kRowsInFlight = sizeof(T) == 2 ? 4 : 2;
   const int lane = threadIdx.x & 31, G = a.group, l = threadIdx.x & (G - 1);
   const int row_lane = threadIdx.x / G, row_lanes = kThreads / G;
   const int64_t o0 = static_cast<int64_t>(blockIdx.x) * G, c0 = o0 * 8;
@@ -333,62 +346,77 @@ __global__ void __launch_bounds__(kThreads) dropout_columns_kernel(const __grid_
   const bool none = a.mask.threshold > 65535u;
   const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
   float acc[8] = {};
-  for (int64_t base = begin; base < end; base += row_lanes * kRowsInFlight) {      // (all lanes of a warp make every trip)
-    if (OCTETS) {
-      const int64_t c = c0 + 8 * l;
-      Octet<T> x[kRowsInFlight];
+  if (OCTETS) {
+    const int64_t c = c0 + 8 * l;
+    if (c + 8 <= a.cols) {
+      // one octet of every row_lanes-th row: pointers and the block number advance by constants, the sums are kept two to an operation
+      const int64_t row0 = begin + row_lane, x_step = row_lanes * a.ldx, y_step = row_lanes * a.ldy;
+      const uint64_t block_step = static_cast<uint64_t>(row_lanes) * static_cast<uint64_t>(a.octets);
+      const T* px = a.x + row0 * a.ldx + c;
+      T* py = a.y + row0 * a.ldy + c;
+      uint64_t block = static_cast<uint64_t>(row0 * a.octets + o0 + l);
+      const uint64_t scale2 = dup2(a.mask.scale);
+      uint64_t acc2[4] = {};
+      auto one = [&](const Octet<T>& x) {
+        uint32_t words[4] = {0, 0, 0, 0};
+        if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
+        float v[8];
+        x.unpack(v);
 #pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) {
-        const int64_t row = base + row_lane + u * row_lanes;
-        if (row < end && c + 8 <= a.cols) x[u].load(a.x + row * a.ldx + c);
-      }
-#pragma unroll
-      for (int u = 0; u < kRowsInFlight; ++u) {
-        const int64_t row = base + row_lane + u * row_lanes;
-        if (row < end && c < a.cols) {
-          const uint64_t block = static_cast<uint64_t>(row * a.octets + o0 + l);
-          if (c + 8 <= a.cols) {
-            uint32_t words[4] = {0, 0, 0, 0};
-            if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
-            float v[8];
-            x[u].unpack(v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              v[j] = masked(v[j], kept(words, j, least), a.mask.scale);
-              acc[j] += v[j];
-            }
-            Storage<T>::store8(a.y + row * a.ldy + c, v);
-          } else {
-            const uint32_t keep = keep_bits(a.mask, block);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              if (c + j < a.cols) {
-                const float v = masked(Storage<T>::load1(a.x + row * a.ldx + c + j), keep >> j & 1, a.mask.scale);
-                acc[j] += v;
-                Storage<T>::store1(a.y + row * a.ldy + c + j, v);
-              }
-            }
-          }
+        for (int j = 0; j < 8; j += 2) {
+          const uint64_t two = mul2(pack2(kept(words, j, least) ? v[j] : 0.0f, kept(words, j + 1, least) ? v[j + 1] : 0.0f), scale2);
+          acc2[j / 2] = add2(acc2[j / 2], two);
+          unpack2(two, v[j], v[j + 1]);
         }
-      }
-    } else {
-      for (int u = 0; u < kRowsInFlight; ++u) {
-        const int64_t row = base + row_lane + u * row_lanes;
-        const bool inside = row < end;
-        T x[8];
+        Storage<T>::store8(py, v);
+        py += y_step;
+        block += block_step;
+      };
+      int n = row0 < end ? static_cast<int>((end - row0 + row_lanes - 1) / row_lanes) : 0;      // (a range has at most 2^31 rows: the grid has its other dimension)
+      for (; n >= kRowsInFlight; n -= kRowsInFlight) {
+        Octet<T> x[kRowsInFlight];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = a.x[min(row, end - 1) * a.ldx + min(c0 + j * G + l, a.cols - 1)];
+        for (int u = 0; u < kRowsInFlight; ++u, px += x_step) x[u].load(px);
+#pragma unroll
+        for (int u = 0; u < kRowsInFlight; ++u) one(x[u]);
+      }
+      for (; n > 0; --n, px += x_step) {
+        Octet<T> x;
+        x.load(px);
+        one(x);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) unpack2(acc2[j], acc[2 * j], acc[2 * j + 1]);
+    } else if (c < a.cols) {                                   // the end of rows that are not whole octets
+      for (int64_t row = begin + row_lane; row < end; row += row_lanes) {
         const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int e = j * G + l;
-          const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
-          const int64_t c = c0 + e;
-          if (inside && c < a.cols) {
-            const float v = masked(Storage<T>::load1(x + j), bits >> (e & 7) & 1, a.mask.scale);
+          if (c + j < a.cols) {
+            const float v = masked(Storage<T>::load1(a.x + row * a.ldx + c + j), keep >> j & 1, a.mask.scale);
             acc[j] += v;
-            Storage<T>::store1(a.y + row * a.ldy + c, v);
+            Storage<T>::store1(a.y + row * a.ldy + c + j, v);
           }
+        }
+      }
+    }
+  } else {
+    for (int64_t base = begin; base < end; base += row_lanes) {      // (all lanes of a warp make every trip)
+      const int64_t row = base + row_lane;
+      const bool inside = row < end;
+      T x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = a.x[min(row, end - 1) * a.ldx + min(c0 + j * G + l, a.cols - 1)];
+      const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e = j * G + l;
+        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, keep, (lane & ~(G - 1)) | (e >> 3));
+        const int64_t c = c0 + e;
+        if (inside && c < a.cols) {
+          const float v = masked(Storage<T>::load1(x + j), bits >> (e & 7) & 1, a.mask.scale);
+          acc[j] += v;
+          Storage<T>::store1(a.y + row * a.ldy + c, v);
         }
       }
     }
@@ -432,14 +460,14 @@ int group_for(int64_t octets) {
 }
 
 // How the rows of a backward pass with column sums are cut: enough ranges for four blocks on each of the 148 multiprocessors, each of
-// at least one trip.  A function of the sizes alone, so that the sums do not depend on the device.
+// at least four rows a thread.  A function of the sizes alone, so that the sums do not depend on the device.
 struct Ranges {
   int64_t count, rows;
 };
 Ranges cut_ranges(int64_t rows, int64_t cols) {
   const int64_t octets = (cols + 7) / 8;
   const int g = group_for(octets);
-  const int64_t strips = (octets + g - 1) / g, trip = static_cast<int64_t>(kThreads / g) * kRowsInFlight;
+  const int64_t strips = (octets + g - 1) / g, trip = static_cast<int64_t>(kThreads / g) * 4;
   const int64_t want = std::max<int64_t>(1, 592 / strips), trips = (rows + trip - 1) / trip;
   Ranges r;
   const int64_t even = (rows + std::min(want, trips) - 1) / std::min(want, trips), lanes = kThreads / g;

@@ -167,7 +167,9 @@ cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
   }
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+  if (e != cudaSuccess) cudaGetLastError();      // (reported by the return value, and not again by whoever asks next)
+  return e;
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -393,7 +393,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) linear_few_kernel(const __grid
 // epilogue has one channel (its scale and bias in registers) and a warp writes 32 neighbouring channels of a token at a time,
 // contiguous for every row length.
 // A tile's inner dimension is cut over a cluster of `split` CTAs when there are fewer tiles than multiprocessors.  Integer sums are exact in
-// any order; each CTA leaves its accumulator in its own shared memory and finishes a share of the tokens by reading the others'.
+// any order; each CTA finishes a share of the tokens, the others write their part of it into slots of its shared memory (which no stage uses:
+// one barrier between the writes and the reads, and nobody has to stay for the others).
 // ---------------------------------------------------------------------------------------------
 constexpr int kTileChannels = 128, kChunk = 128;           // rows of the weights' box, bytes (= codes) of a stage's rows
 constexpr int kTileThreads = 320;                          // TMA producer, MMA issuer, eight epilogue warps
@@ -433,10 +434,14 @@ __device__ __forceinline__ uint32_t peer_smem(uint32_t addr, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ int lds_peer(uint32_t addr) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void sts_peer(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap& map) { asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory"); }
+// The sum of a cluster's CTAs for one token and channel, from the slots that they have filled in this CTA's shared memory.
+__device__ __forceinline__ uint32_t sum_of_slots(uint32_t at, uint32_t slot_bytes, int split) {
+  uint32_t v[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[r]) : "r"(at + min(r, split - 1) * slot_bytes) : "memory");
+  return v[0] + v[1] + (split > 2 ? v[2] + v[3] : 0u);
 }
 
 // The epilogue of U tokens (8 or 16) of one channel per lane; a warp's lanes hold 32 consecutive channels from a multiple of 32.
@@ -511,8 +516,13 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   const int last = static_cast<int>(static_cast<int64_t>(chunks) * (rank + 1) / shape.split);
   const uint32_t stage_bytes = kTileChannels * kChunk + shape.tokens * kChunk;
   const uint32_t tmem_cols = shape.tokens <= 32 ? 32 : (shape.tokens <= 64 ? 64 : (shape.tokens <= 128 ? 128 : 256));
+  // the cluster's sums: groups of eight tokens, two by two to the CTAs in turn; a slot for each source
+  const int groups = shape.tokens / 8, own_groups = (groups / 2 + shape.split - 1) / shape.split * 2;
+  const uint32_t sums0 = stages0 + shape.stages * stage_bytes, slot_bytes = own_groups * 8 * kTileChannels * 4;
   volatile int* aborted = &abort_flag;
   if (threadIdx.x == 0) {
+    prefetch_map(map_w);
+    prefetch_map(map_x);
     abort_flag = 0;
     for (int s = 0; s < shape.stages; ++s) {
       mbar_init(smem_u32(&full[s]), 1);
@@ -528,6 +538,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (shape.split > 1) cluster_arrive();                    // (waited for before anybody writes into another's shared memory)
   const uint32_t tmem = tmem_slot;
   bool ok = true;
   if (warp == 0) {
@@ -611,38 +622,38 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     }
   }
   if (shape.split > 1) {
-    // [token][channel], over the stages, which nothing uses any more
+    __syncwarp();
+    cluster_wait();
+    const uint32_t channel = (quarter * 32 + lane) * 4;
     if (warp >= 2 && ok) {
-      for (int g = half; g < shape.tokens / 8; g += 2) {
+      for (int g = half; g < groups; g += 2) {
         uint32_t v[8];
         tmem_ld8(mine + g * 8, v);
+        const int owner = (g >> 1) % shape.split, place = (g >> 1) / shape.split * 2 + (g & 1);
+        const uint32_t to = peer_smem(sums0 + rank * slot_bytes + place * 8 * kTileChannels * 4 + channel, owner);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sts32(stages0 + ((g * 8 + j) * kTileChannels + quarter * 32 + lane) * 4, v[j]);
+        for (int j = 0; j < 8; ++j) sts_peer(to + j * kTileChannels * 4, v[j]);
       }
     }
     __syncwarp();
     cluster_arrive();
     cluster_wait();
     if (warp >= 2) {
-      for (int g = static_cast<int>(rank) * 2 + half; g < shape.tokens / 8 && m0 + g * 8 < a.m; g += shape.split * 2) {
-        uint32_t sum[8] = {};
+      for (int place = half; place < own_groups; place += 2) {
+        const int g = ((place >> 1) * shape.split + static_cast<int>(rank)) * 2 + (place & 1);
+        if (g >= groups || m0 + g * 8 >= a.m) break;
         T add[8];
         if (a.residual) residual_ahead<T, 8>(a, m0 + g * 8, n, add);
-        for (int r = 0; r < shape.split; ++r) {
-          const uint32_t from = peer_smem(stages0 + (g * 8 * kTileChannels + quarter * 32 + lane) * 4, r);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) sum[j] += static_cast<uint32_t>(lds_peer(from + j * kTileChannels * 4));
-        }
         float sx[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sx[j] = a.sx[min(m0 + g * 8 + j, a.m - 1)];
+        uint32_t sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = sum_of_slots(sums0 + (place * 8 + j) * kTileChannels * 4 + channel, slot_bytes, shape.split);
         finish<T, DROP, 8>(a, sum, sx, m0 + g * 8, n, sw, bias, add);
       }
     }
-    __syncwarp();
-    cluster_arrive();                                       // no CTA leaves while another reads its sums
-    cluster_wait();
   }
   tc_fence_before();
   __syncthreads();
@@ -710,6 +721,8 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
   const int half_tokens = shape.tokens / 2;
   volatile int* aborted = &abort_flag;
   if (threadIdx.x == 0) {
+    prefetch_map(map_w);
+    prefetch_map(map_x);
     abort_flag = 0;
     for (int s = 0; s < kPairStages; ++s) {
       mbar_init(smem_u32(&full[s]), 1);
@@ -898,6 +911,7 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
 // do 128 * 48 products a cycle, a token of the epilogue costs 25 cycles, sums that travel between CTAs 600 a CTA and 12 a token.  One CTA on a
 // multiprocessor with all of its shared memory as stages is better than two, and pairs are better than several rounds of single CTAs.
 constexpr int kTileSmem = 110 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
+int tile_sums_bytes(const TileShape& s) { return s.split > 1 ? (s.tokens / 16 + s.split - 1) / s.split * 16 * s.split * kTileChannels * 4 : 0; }
 // copies beside products: the longer of the two, and some of the other (both draw on the same power)
 double overlapped(double a, double b) { return std::max(a, b) + 0.3 * std::min(a, b); }
 TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
@@ -917,7 +931,8 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
       const double cost = steady * each + ends * ((each + 1) / 2) + (each > 1 ? 1500 : 0);
       if (best.tokens == 0 || cost < least) {
         const int stage = (kTileChannels + s.tokens) * kChunk;
-        s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024) / stage);
+        s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024 - tile_sums_bytes(s)) / stage);
+        if (s.stages < 2) continue;
         best = s;
         least = cost;
       }
@@ -938,10 +953,7 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
   }
   return best;
 }
-int tile_smem_bytes(const TileShape& s) {
-  const int stages = s.stages * (kTileChannels + s.tokens) * kChunk, sums = s.split > 1 ? s.tokens * kTileChannels * 4 : 0;
-  return std::max(stages, sums) + 1024;
-}
+int tile_smem_bytes(const TileShape& s) { return s.stages * (kTileChannels + s.tokens) * kChunk + tile_sums_bytes(s) + 1024; }
 
 template <typename T, bool DROP>
 cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
