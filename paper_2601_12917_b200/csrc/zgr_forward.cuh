@@ -53,10 +53,11 @@ struct Octet {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
   }
-  // (read again and again, by many threads)
+  // Read again and again, by many threads: kept in L1.  (Not by the read-only path: a kernel that was launched early may have begun before the
+  // kernel in front wrote what it reads.)
   __device__ __forceinline__ void load_shared(const T* p) {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldca(reinterpret_cast<const uint4*>(p) + i);
   }
   __device__ __forceinline__ void zero() {
 #pragma unroll
@@ -78,7 +79,7 @@ struct Octet {
     uint32_t g[kWords + 4];
 #pragma unroll
     for (int i = 0; i < kWords / 4 + 1; ++i) {
-      const uint4 q = __ldg(base + i);
+      const uint4 q = __ldca(base + i);
       g[4 * i] = q.x, g[4 * i + 1] = q.y, g[4 * i + 2] = q.z, g[4 * i + 3] = q.w;
     }
     const bool two = at & 8, one = at & 4, half = at & 2;

@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(ROWS == 4 ? 128 : 384) quantize_rows_kernel(co
 // Rows of more than 18432 elements: read twice, a block a row.
 constexpr int64_t kLongRow = 18432;
 template <typename T>
-__global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* __restrict__ x, const int64_t ldx, const int64_t cols, int8_t* __restrict__ codes,
-                                                                 const int64_t ldc, float* __restrict__ scales, const int early) {
+__global__ void __launch_bounds__(512) quantize_long_rows_kernel(const T* x, const int64_t ldx, const int64_t cols, int8_t* codes,
+                                                                 const int64_t ldc, float* scales, const int early) {
   __shared__ uint32_t part[16];
   dependency_wait();
   if (early) dependents_may_start();

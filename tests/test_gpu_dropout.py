@@ -1,9 +1,12 @@
 """Dropout from the counter-based generator: forward, backward, the bias's gradient, against the 64-bit form; layouts, masks, graphs, refusals."""
+import threading
+
 import numpy as np
 import pytest
 import torch
 
 import forward_ref as ref
+import oracle
 from paper_2601_12917_b200 import zgr
 
 pytestmark = pytest.mark.gpu
@@ -175,3 +178,57 @@ def test_binding_refuses():
         assert e.value.code == zgr.EINVAL
     with pytest.raises(zgr.ZgrError):
         zgr.dropout(x[:1].expand(4, 16), 0.1, 1)         # rows on top of each other
+
+
+@pytest.mark.parametrize("cols", [61440, 61441])
+def test_offsets_past_32_bits(cols):
+    # more than 2^32 elements: the last rows against the generator's blocks for them (octets by a 64-bit division from 2^31 on)
+    rows = (1 << 32) // cols + 3
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 1 << 32
+    y = zgr.dropout(x, 0.5, 21, 3, out=x)
+    octets = (cols + 7) // 8
+    for row in (0, 35000, rows - 2, rows - 1):
+        words = np.asarray(oracle.blocks(21, 3, ref.TAG_DROPOUT, row * octets, octets)).astype(np.uint32).reshape(-1, 4)
+        keep = np.stack([words & 0xFFFF, words >> 16], axis=2).reshape(-1)[:cols] >= 32768
+        assert np.array_equal(y[row].float().cpu().numpy(), np.where(keep, 2.0, 0.0))
+
+
+def test_a_chain_of_launches_sees_what_is_in_front_of_it():
+    # every call starts while the one in front ends, and works in place on what that one writes: the same as with a wait behind each
+    def chain(wait):
+        x = make((37, 1021), "f32", 5)
+        b = make((1021,), "f32", 6)
+        for i in range(60):
+            zgr.dropout(x, 0.05, i, bias=b, out=x)
+            if wait:
+                torch.cuda.synchronize()
+            d, b = zgr.dropout_backward(x, 0.1, i, bias_grad=True, out=x)
+            if wait:
+                torch.cuda.synchronize()
+            zgr.dropout(d, 0.2, i, 1, residual=d, out=x)
+            x.mul_(0.5)
+            b.mul_(0.1)
+        return x, b
+    quick, slow = chain(False), chain(True)
+    assert torch.equal(quick[0], slow[0]) and torch.equal(quick[1], slow[1])
+
+
+def test_calls_from_several_threads():
+    want = [zgr.dropout(make((64, 999), "f16", i), 0.3, i) for i in range(4)]
+    torch.cuda.synchronize()
+    got, streams = [[] for _ in range(4)], [torch.cuda.Stream() for _ in range(4)]
+
+    def work(i):
+        x = make((64, 999), "f16", i)
+        torch.cuda.synchronize()
+        for _ in range(50):
+            got[i].append(zgr.dropout(x, 0.3, i, stream=streams[i]))
+        streams[i].synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for w, ys in zip(want, got):
+        assert len(ys) == 50 and all(torch.equal(w, y) for y in ys)

@@ -249,3 +249,36 @@ def test_empty_batches_and_refusals():
         with pytest.raises(zgr.ZgrError) as e:
             bad()
         assert e.value.code == zgr.EINVAL
+
+
+def test_a_chain_of_launches_sees_what_is_in_front_of_it():
+    # weights requantised and tokens replaced between products whose launches overlap: the same as with a wait behind each.  The product
+    # fetches weights before it waits for its tokens' quantiser; they may have been written by the call in front of that.
+    def chain(m, wait):
+        w, h = make((640, 640), "bf16", 1, 0.04), make((m, 640), "bf16", 2)
+        for i in range(25):
+            wq, ws = zgr.quantize_rows(w)
+            if wait:
+                torch.cuda.synchronize()
+            h = zgr.linear_i8(h, wq, ws, residual=h, p=0.1, seed=i)
+            if wait:
+                torch.cuda.synchronize()
+            zgr.dropout(w, 0.01, i, 7, out=w)
+            h = h / h.float().std()
+            h = h.bfloat16()
+        return h
+    for m in (1, 2, 9, 64, 700):
+        assert torch.equal(chain(m, False), chain(m, True)), m
+
+
+def test_rows_behind_each_other_at_large_offsets():
+    # 2^32 results in front of the last rows: only a few rows of them are looked at
+    k, n, m = 64, 70000, 62000
+    x = make((128, k), "bf16").repeat((m + 127) // 128, 1)[:m]
+    wq, ws = zgr.quantize_rows(make((n, k), "bf16", 1))
+    y = zgr.linear_i8(x, wq, ws)
+    assert y.numel() > 1 << 32
+    small = zgr.linear_i8(x[:128], wq, ws)
+    for row in (0, 30000, 61500, m - 1):
+        assert torch.equal(y[row], small[row % 128])
+    assert zgr.linear_status() == 0
