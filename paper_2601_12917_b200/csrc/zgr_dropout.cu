@@ -63,26 +63,27 @@ __device__ __forceinline__ float masked_plus(float v, bool keep, float scale, fl
 // FLAT: the matrices are whole octets without gaps and there is no bias, so that octet i of the tensor lies at element 8 i.
 // What bounds it beside the memory is the number of instructions: an octet may cost about 250 issue slots of its scheduler before they are
 // longer than the traffic of a residual sum, the generator's rounds take 40, and this form needs about 110.
-template <typename T, int U, bool FLAT>
+template <typename T, int U, bool FLAT, typename Index>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ DropArgs<T> a) {
   Octet<T> x[U], r[U];
-  int64_t at[U], row[U];
+  int64_t at[U];
+  Index row[U];
   int col[U];
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads * U) + threadIdx.x;
+  const Index first = static_cast<Index>(blockIdx.x) * (kThreads * U) + threadIdx.x, total = static_cast<Index>(a.total);
   const int cols = static_cast<int>(a.cols);                   // (below 2^31 unless FLAT)
   dependency_wait();
-  const int64_t left = a.total - first;                        // octet u exists if u * kThreads < left
+  const Index left = first < total ? total - first : 0;        // octet u exists if u * kThreads < left
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (u * kThreads < left) {
+    if (static_cast<Index>(u * kThreads) < left) {
       if (FLAT) {
-        at[u] = (first + u * kThreads) * 8;
+        at[u] = static_cast<int64_t>(first + u * kThreads) * 8;
         x[u].load(a.x + at[u]);
         if (a.residual) r[u].load(a.residual + at[u]);
       } else {
-        const int64_t i = first + u * kThreads;
-        row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.pieces;
-        col[u] = static_cast<int>(i - row[u] * a.pieces) * 8;
+        const Index i = first + u * kThreads;
+        row[u] = sizeof(Index) == 4 ? fast_div(static_cast<uint32_t>(i), a.div) : i / a.pieces;
+        col[u] = static_cast<int>(i - row[u] * static_cast<Index>(a.pieces)) * 8;
         if (col[u] + 8 <= cols) {
           x[u].load(a.x + row[u] * a.ldx + col[u]);
           if (a.residual) r[u].load(a.residual + row[u] * a.ldr + col[u]);
@@ -97,10 +98,9 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
   const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (u * kThreads < left) {
+    if (static_cast<Index>(u * kThreads) < left) {
       uint32_t words[4] = {0, 0, 0, 0};
-      const uint64_t block = static_cast<uint64_t>(first + u * kThreads);
-      if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
+      if (!none) block_words(a.mask, first + u * kThreads, words);
       float v[8];
       x[u].unpack(v);
       if (!FLAT && a.bias) {
@@ -141,21 +141,22 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
 // eight elements wherever a row ends, so that all accesses are whole and aligned; a piece from column c on takes its bits from the block
 // of c, made here, from the next piece's, got from the next lane, and, where the row ends within it, sometimes from a third, made by that lane
 // alone.  fp16, 16336 x 1021: 27.8 us by the rows' own pieces (dropout_shifted_kernel), whose ends are loaded and stored element by element.
-template <typename T, int U>
+// Index: 32 bits where the tensor has fewer than 2^31 elements (issue slots are what bounds it).
+template <typename T, int U, typename Index>
 __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid_constant__ DropArgs<T> a) {
   const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
   dependency_wait();
-  const int64_t elements = a.rows * a.cols;
-  const int64_t first = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
+  const Index elements = static_cast<Index>(a.rows * a.cols), total = static_cast<Index>(a.total), octets = static_cast<Index>(a.octets);
+  const Index first = (static_cast<Index>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
   Octet<T> x[U], r[U];
-  int64_t row[U];
+  Index row[U];
   int col[U];
   uint32_t own[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = min(first + u * 32, a.total - 1), e = i * 8;
-    row[u] = elements < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(e), a.div)) : e / a.cols;
-    col[u] = static_cast<int>(e - row[u] * a.cols);
+    const Index e = min(first + u * 32, total - 1) * 8;
+    row[u] = sizeof(Index) == 4 ? fast_div(static_cast<uint32_t>(e), a.div) : e / a.cols;
+    col[u] = static_cast<int>(e - row[u] * static_cast<Index>(a.cols));
     if (e + 8 <= elements) {
       x[u].load(a.x + e);
       if (a.residual) r[u].load(a.residual + e);
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
     }
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) own[u] = keep_bits(a.mask, static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3)));
+  for (int u = 0; u < U; ++u) own[u] = keep_bits(a.mask, row[u] * octets + (col[u] >> 3));
   // the block behind a warp's pieces is the next warp's first; only behind the last warp's it is made once more
   __shared__ uint32_t firsts[kThreads / 32];
   const int warp = threadIdx.x >> 5;
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = first + u * 32;
+    const Index i = first + u * 32;
     // the next piece's block: of this row, or the first of the next
     uint32_t next = __shfl_down_sync(0xFFFFFFFFu, own[u], 1);
     if (u + 1 < U) {
@@ -181,20 +182,20 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
       if (lane == 31) next = over;
     }
     const int s = col[u] & 7, left = cols - col[u];            // elements of the row from here on
-    const uint64_t block = static_cast<uint64_t>(row[u] * a.octets + (col[u] >> 3));
+    const Index block = row[u] * octets + (col[u] >> 3);
     if (u + 1 == U) {
       if (warp + 1 < kThreads / 32) {
         const uint32_t over = firsts[warp + 1];
         if (lane == 31) next = over;
       } else if (lane == 31) {
-        next = keep_bits(a.mask, left > 8 ? block + 1 : static_cast<uint64_t>((row[u] + 1) * a.octets));
+        next = keep_bits(a.mask, left > 8 ? block + 1 : (row[u] + 1) * octets);
       }
     }
     uint32_t rest = next;                                      // behind this block in the same row
     if (left <= 8 && left > 8 - s) rest = keep_bits(a.mask, block + 1);
     uint32_t keep = own[u] >> s | rest << (8 - s);
     if (left < 8) keep = (keep & ((1u << left) - 1)) | next << left;
-    if (i < a.total) {
+    if (i < total) {
       float v[8];
       x[u].unpack(v);
       if (a.bias) {
@@ -229,20 +230,21 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
 // elements before it, at the boundary, and take the last s bits of one generator block and the first 8 - s of the next: a thread
 // makes the block of its own piece and gets its neighbour's bits from the neighbouring lane; a warp's pieces follow each other, so that only its
 // first lane makes a second block, once for U pieces.
-template <typename T, int U>
+template <typename T, int U, typename Index>
 __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_constant__ DropArgs<T> a) {
   constexpr int kPhases = 16 / sizeof(T);
   const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
   dependency_wait();
   Octet<T> x[U], r[U];
-  int64_t row[U];
+  Index row[U];
   int piece[U], shift[U];
-  const int64_t first = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
+  const Index total = static_cast<Index>(a.total), octets = static_cast<Index>(a.octets);
+  const Index first = (static_cast<Index>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * (32 * U) + lane;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t i = min(first + u * 32, a.total - 1);
-    row[u] = a.total < (int64_t{1} << 31) ? static_cast<int64_t>(fast_div(static_cast<uint32_t>(i), a.div)) : i / a.pieces;
-    piece[u] = static_cast<int>(i - row[u] * a.pieces);
+    const Index i = min(first + u * 32, total - 1);
+    row[u] = sizeof(Index) == 4 ? fast_div(static_cast<uint32_t>(i), a.div) : i / a.pieces;
+    piece[u] = static_cast<int>(i - row[u] * static_cast<Index>(a.pieces));
     shift[u] = static_cast<int>((static_cast<uint32_t>(a.phase) + static_cast<uint32_t>(row[u]) * static_cast<uint32_t>(a.ldx)) & (kPhases - 1));      // (only the low bits count)
     const int col = piece[u] * 8 - shift[u];
     if (col >= 0 && col + 8 <= cols) {
@@ -256,13 +258,13 @@ __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_
   uint32_t before = 0;   // lane 31's block of the pieces before
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint64_t block = static_cast<uint64_t>(row[u] * a.octets + piece[u]);
+    const Index block = row[u] * octets + piece[u];
     const uint32_t own = keep_bits(a.mask, block);
     uint32_t left = __shfl_up_sync(0xFFFFFFFFu, own, 1);
     if (lane == 0) left = u > 0 ? before : (piece[u] > 0 ? keep_bits(a.mask, block - 1) : 0u);
     if (U > 1) before = __shfl_sync(0xFFFFFFFFu, own, 31);
     const uint32_t keep = (own << 8 | left) >> (8 - shift[u]);
-    if (first + u * 32 < a.total) {
+    if (first + u * 32 < total) {
       const int col = piece[u] * 8 - shift[u];
       float v[8];
       x[u].unpack(v);
@@ -333,7 +335,7 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
 // (an octet, or the elements l, l + G, ... where rows start anywhere) whose sums it keeps in fp32.  The sums of a block meet in shared
 // memory, those of the ranges in the workspace, and column_sums_kernel adds them in a fixed order: the same bits every time.
 // Four blocks on a multiprocessor, for which the grid is cut (cut_ranges): with 80 registers it was three, and a third of a second round.
-template <typename T, bool OCTETS>
+template <typename T, bool OCTETS, typename Index>
 __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials) {
   __shared__ float sums[kThreads * 8];
   constexpr int kRowsInFlight = sizeof(T) == 2 ? 4 : 2;
@@ -351,15 +353,15 @@ __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __gr
     if (c + 8 <= a.cols) {
       // one octet of every row_lanes-th row: pointers and the block number advance by constants, the sums are kept two to an operation
       const int64_t row0 = begin + row_lane, x_step = row_lanes * a.ldx, y_step = row_lanes * a.ldy;
-      const uint64_t block_step = static_cast<uint64_t>(row_lanes) * static_cast<uint64_t>(a.octets);
+      const Index block_step = static_cast<Index>(row_lanes) * static_cast<Index>(a.octets);
       const T* px = a.x + row0 * a.ldx + c;
       T* py = a.y + row0 * a.ldy + c;
-      uint64_t block = static_cast<uint64_t>(row0 * a.octets + o0 + l);
+      Index block = static_cast<Index>(row0 * a.octets + o0 + l);
       const uint64_t scale2 = dup2(a.mask.scale);
       uint64_t acc2[4] = {};
       auto one = [&](const Octet<T>& x) {
         uint32_t words[4] = {0, 0, 0, 0};
-        if (!none) keep_words(a.mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), words);
+        if (!none) block_words(a.mask, block, words);
         float v[8];
         x.unpack(v);
 #pragma unroll
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __gr
       for (int j = 0; j < 4; ++j) unpack2(acc2[j], acc[2 * j], acc[2 * j + 1]);
     } else if (c < a.cols) {                                   // the end of rows that are not whole octets
       for (int64_t row = begin + row_lane; row < end; row += row_lanes) {
-        const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+        const uint32_t keep = keep_bits(a.mask, static_cast<Index>(row * a.octets + o0 + l));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (c + j < a.cols) {
@@ -407,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __gr
       T x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = a.x[min(row, end - 1) * a.ldx + min(c0 + j * G + l, a.cols - 1)];
-      const uint32_t keep = keep_bits(a.mask, static_cast<uint64_t>(row * a.octets + o0 + l));
+      const uint32_t keep = keep_bits(a.mask, static_cast<Index>(row * a.octets + o0 + l));
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int e = j * G + l;
@@ -499,10 +501,15 @@ int run_dropout(DropArgs<T> a, cudaStream_t st) {
     const bool small = a.total < int64_t{148} * 8 * kThreads;
     const int64_t per_block = kThreads * (small ? 1 : kMany), blocks = (a.total + per_block - 1) / per_block;
     if (blocks > 0x7FFFFFFF) return ZGR_ETOOBIG;
-    const auto kernel = unbroken ? (small ? dropout_unbroken_kernel<T, 1> : dropout_unbroken_kernel<T, kMany>)
-                        : shift ? (small ? dropout_shifted_kernel<T, 1> : dropout_shifted_kernel<T, kMany>)
-                        : flat ? (small ? dropout_kernel<T, 1, true> : dropout_kernel<T, kMany, true>)
-                               : (small ? dropout_kernel<T, 1, false> : dropout_kernel<T, kMany, false>);
+    const bool far = (unbroken ? a.rows * a.cols : a.total) >= int64_t{1} << 31;      // indexes of 64 bits
+    const auto kernel = far ? (unbroken ? dropout_unbroken_kernel<T, kMany, int64_t>
+                               : shift  ? dropout_shifted_kernel<T, kMany, int64_t>
+                               : flat   ? dropout_kernel<T, kMany, true, int64_t>
+                                        : dropout_kernel<T, kMany, false, int64_t>)
+                        : unbroken ? (small ? dropout_unbroken_kernel<T, 1, uint32_t> : dropout_unbroken_kernel<T, kMany, uint32_t>)
+                        : shift ? (small ? dropout_shifted_kernel<T, 1, uint32_t> : dropout_shifted_kernel<T, kMany, uint32_t>)
+                        : flat ? (small ? dropout_kernel<T, 1, true, uint32_t> : dropout_kernel<T, kMany, true, uint32_t>)
+                               : (small ? dropout_kernel<T, 1, false, uint32_t> : dropout_kernel<T, kMany, false, uint32_t>);
     return launch_behind(kernel, static_cast<unsigned>(blocks), kThreads, 0, 1, st, a) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
   }
   a.group = group_for(a.octets);
@@ -521,7 +528,10 @@ int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st)
   if (strips > 0x7FFFFFFF || r.count > 65535) return ZGR_ETOOBIG;
   const dim3 grid(static_cast<unsigned>(strips), static_cast<unsigned>(r.count));
   const bool octets = octets_aligned(a.x, a.rows, a.ldx, sizeof(T)) && octets_aligned(a.y, a.rows, a.ldy, sizeof(T));
-  if (launch_behind(octets ? dropout_columns_kernel<T, true> : dropout_columns_kernel<T, false>, grid, kThreads, 0, 1, st, a, r.rows, partials) != cudaSuccess)
+  const bool far = a.rows * a.octets >= int64_t{1} << 32;      // block numbers of 64 bits
+  const auto kernel = far ? (octets ? dropout_columns_kernel<T, true, uint64_t> : dropout_columns_kernel<T, false, uint64_t>)
+                          : (octets ? dropout_columns_kernel<T, true, uint32_t> : dropout_columns_kernel<T, false, uint32_t>);
+  if (launch_behind(kernel, grid, kThreads, 0, 1, st, a, r.rows, partials) != cudaSuccess)
     return ZGR_ECUDA;
   const cudaError_t e = launch_behind(column_sums_kernel<T>, static_cast<unsigned>((a.cols + 31) / 32), dim3(32, 8), 0, 1, st, partials, static_cast<int>(r.count), a.cols, dbias);
   return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;

@@ -32,11 +32,18 @@ __device__ __forceinline__ void keep_words(const DropMask& mask, uint32_t lo, ui
 }
 __device__ __forceinline__ bool kept(const uint32_t (&x)[4], int i, uint32_t least) { return (i & 1 ? x[i >> 1] : x[i >> 1] << 16) >= least; }
 
+// (A block number of 32 bits leaves out the form for the others.)
+template <typename Block>
+__device__ __forceinline__ void block_words(const DropMask& mask, Block block, uint32_t (&x)[4]) {
+  keep_words(mask, static_cast<uint32_t>(block), sizeof(Block) > 4 ? static_cast<uint32_t>(static_cast<uint64_t>(block) >> 32) : 0u, x);
+}
+
 // Bit i of the result: element 8 o + i of the row is kept.
-__device__ __forceinline__ uint32_t keep_bits(const DropMask& mask, uint64_t block) {
+template <typename Block>
+__device__ __forceinline__ uint32_t keep_bits(const DropMask& mask, Block block) {
   if (mask.threshold > 65535u) return 0;
   uint32_t x[4];
-  keep_words(mask, static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), x);
+  block_words(mask, block, x);
   const uint32_t least = keep_least(mask);
   uint32_t bits = 0;
 #pragma unroll
