@@ -50,13 +50,14 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 
 // A row is read once and stays in registers between the two passes over it, NV octets a thread, as few as hold it (idle lanes cost as much as
 // the others).  ROWS = 4: four warps a block with a row each, up to 1536 elements; ROWS = 1: a block a row, with four, eight or twelve
-// warps, at most six octets a thread.  4096 rows of 11008 bf16 elements: 27 us with eight warps and six octets, 34 with sixteen and three
-// or with eleven and four.
+// warps, at most six octets a thread; 16-bit rows in as few registers as leave room for three blocks of 384 threads.  4096 rows of 11008
+// bf16 elements: 26 us (5.2 TB/s; 29 without that bound, 34 with sixteen warps and three octets or with eleven and four), 13824 of 5120 35 us
+// (6.0 TB/s), 4096 of 4096 10.2 us.  Bound by memory and, in the last, by one wave of blocks that all load, reduce and store at once.
 // The rows of x may start anywhere (ALIGNED = false: octets are put together from 16-byte granules, one by one at the row's ends), as may
 // those of the codes (`wide` = 0: written byte by byte).
 // early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not.
 template <typename T, int ROWS, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(ROWS == 4 ? 128 : 384) quantize_rows_kernel(const T* x, const int64_t ldx, const int64_t rows, const int cols, int8_t* codes,
+__global__ void __launch_bounds__(ROWS == 4 ? 128 : 384, ALIGNED && sizeof(T) == 2 && ROWS == 1 ? 3 : 1) quantize_rows_kernel(const T* x, const int64_t ldx, const int64_t rows, const int cols, int8_t* codes,
                                                                               const int64_t ldc, float* scales, const int wide, const int early) {
   __shared__ uint32_t part[16];
   dependency_wait();

@@ -149,7 +149,8 @@ def _stream_ptr(stream) -> Optional[int]:
 
 # -- operators of the forward pass --------------------------------------------------------------------------------
 # Their marshalling is a compiled module (csrc/zgr_bind.cpp), built beside the library: they last a few microseconds on the device, and
-# ctypes with the checks around it took as long.  It calls the functions of the library loaded above.
+# ctypes with the checks around it took as long.  It calls the functions of the library loaded above.  Nothing here is recorded by
+# autograd: the backward pass is a call of its own, under the same (p, seed, tensor).
 _STORAGE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _bind = None
 

@@ -180,6 +180,11 @@ def test_binding_refuses():
         zgr.dropout(x[:1].expand(4, 16), 0.1, 1)         # rows on top of each other
 
 
+def keep_blocks(seed, tensor, first, n):
+    words = np.asarray(oracle.blocks(seed, tensor, ref.TAG_DROPOUT, first, n)).astype(np.uint32).reshape(-1, 4)
+    return np.stack([words & 0xFFFF, words >> 16], axis=2).reshape(-1) >= 32768
+
+
 @pytest.mark.parametrize("cols", [61440, 61441])
 def test_offsets_past_32_bits(cols):
     # more than 2^32 elements: the last rows against the generator's blocks for them (octets by a 64-bit division from 2^31 on)
@@ -189,9 +194,19 @@ def test_offsets_past_32_bits(cols):
     y = zgr.dropout(x, 0.5, 21, 3, out=x)
     octets = (cols + 7) // 8
     for row in (0, 35000, rows - 2, rows - 1):
-        words = np.asarray(oracle.blocks(21, 3, ref.TAG_DROPOUT, row * octets, octets)).astype(np.uint32).reshape(-1, 4)
-        keep = np.stack([words & 0xFFFF, words >> 16], axis=2).reshape(-1)[:cols] >= 32768
-        assert np.array_equal(y[row].float().cpu().numpy(), np.where(keep, 2.0, 0.0))
+        assert np.array_equal(y[row].float().cpu().numpy(), np.where(keep_blocks(21, 3, row * octets, octets)[:cols], 2.0, 0.0))
+
+
+@pytest.mark.parametrize("cols", [(1 << 31) + 64, (1 << 31) + 13])
+def test_rows_longer_than_31_bits(cols):
+    x = torch.ones(cols, dtype=torch.float16, device="cuda")
+    b = torch.zeros(cols, dtype=torch.float16, device="cuda") if cols % 8 == 0 else None
+    for bias in (None, b) if b is not None else (None,):
+        y = zgr.dropout(x, 0.5, 4, 2, bias=bias)
+        last = (cols + 7) // 8 - 100
+        keep = keep_blocks(4, 2, last, 100)[:cols - 8 * last]
+        assert np.array_equal(y[8 * last:].float().cpu().numpy(), np.where(keep, 2.0, 0.0))
+        assert np.array_equal(y[:800].float().cpu().numpy(), np.where(keep_blocks(4, 2, 0, 100), 2.0, 0.0))
 
 
 def test_a_chain_of_launches_sees_what_is_in_front_of_it():
