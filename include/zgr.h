@@ -386,11 +386,11 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
  * of the weights (after a sweep: of the perturbed ones).  D is the dropout of zgr_dropout with cols = n (p = 0: nothing).
  * The sums are exact.  A token that holds an infinity or a NaN gives NaN in its row (where it is not dropped).
  * w: 16-byte aligned, ldw a multiple of 16 (what lies behind the k-th code of a row is not used).  k at most 2^17.  m may be 0.
- * workspace: 16-byte aligned, at least zgr_linear_i8_workspace(m, k) bytes (0 for a few tokens, and it may be NULL then): the tokens'
+ * workspace: 16-byte aligned, at least zgr_linear_i8_workspace(m, n, k) bytes (0 for a few tokens, and it may be NULL then): the tokens'
  * codes and scales.  Its contents before the call do not matter.
  * ZGR_EINVAL: null or misaligned pointer, size out of range, ld below the row, unknown dtype, p outside [0, 1], workspace missing,
  * misaligned or too small. */
-int64_t zgr_linear_i8_workspace(int64_t m, int64_t k);
+int64_t zgr_linear_i8_workspace(int64_t m, int64_t n, int64_t k);
 int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias, const void* residual, int64_t ldr, void* y,
                   int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* workspace,
                   int64_t workspace_bytes, void* stream);

@@ -261,7 +261,7 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Matrix m = matrix_of(x, "x");
     const Product p = product_of(here, a + 1, type, x, m.cols);
     at::Tensor workspace;
-    const int64_t bytes = f_linear_i8_workspace(m.rows, m.cols);      // (negative: a size that the call itself refuses)
+    const int64_t bytes = f_linear_i8_workspace(m.rows, p.w.rows, m.cols);      // (negative: a size that the call itself refuses)
     if (bytes > 0) workspace = empty({bytes}, at::kByte, here);
     check(f_linear_i8(m.data, m.ld, static_cast<const int8_t*>(p.w.data), p.w.ld, p.w_scale, p.bias, p.residual.data, p.residual.ld, p.y.data, p.y.ld, m.rows, p.w.rows,
                       m.cols, storage, p.p, p.seed, p.tensor, bytes > 0 ? workspace.data_ptr() : nullptr, bytes > 0 ? bytes : 0, here.stream()));

@@ -56,9 +56,11 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 // The rows of x may start anywhere (ALIGNED = false: octets are put together from 16-byte granules, one by one at the row's ends), as may
 // those of the codes (`wide` = 0: written byte by byte).
 // early: the kernel behind this one is the library's product, which may start and wait; the caller's own kernels may not.
+constexpr int row_threads(int rows) { return rows == 4 ? 128 : 384; }
 template <typename T, int ROWS, int NV, bool ALIGNED>
-__global__ void __launch_bounds__(ROWS == 4 ? 128 : 384, ALIGNED && sizeof(T) == 2 && ROWS == 1 ? 3 : 1) quantize_rows_kernel(const T* x, const int64_t ldx, const int64_t rows, const int cols, int8_t* codes,
-                                                                              const int64_t ldc, float* scales, const int wide, const int early) {
+__global__ void __launch_bounds__(row_threads(ROWS), ALIGNED && sizeof(T) == 2 && ROWS == 1 ? 3 : 1)
+    quantize_rows_kernel(const T* x, const int64_t ldx, const int64_t rows, const int cols, int8_t* codes, const int64_t ldc, float* scales, const int wide,
+                         const int early) {
   __shared__ uint32_t part[16];
   dependency_wait();
   if (early) dependents_may_start();
@@ -204,14 +206,15 @@ __device__ __forceinline__ float finish1(int sum, float sx, float sw, float bias
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few tokens (one or two): the weights are read once and nothing else counts.  A block on every multiprocessor; each warp takes channels in turn and
+// Few tokens (up to eight): the weights are read once and nothing else counts.  A block on every multiprocessor; each warp takes channels in turn and
 // streams their codes through slots of its own in shared memory: one lane starts bulk copies of up to 4096 bytes, two to eight of them
 // ahead (about 190 KB in flight on a multiprocessor, whatever the number of registers), all lanes multiply them with the tokens' codes, four
-// products an instruction.  The sums of 32 channels wait in the 32 lanes for one epilogue.  Every block quantises the tokens for itself while its first weights are on their way: one launch, no workspace.
-// With the loads in registers, eight a lane, the issue slots showed (30 to 70 instructions a load): 12.4 us for 4096 -> 11008 and 15.5 us for
-// 11008 -> 4096, 7.0 of them for the bytes.
+// products an instruction.  The sums of 32 channels wait in the 32 lanes for one epilogue.  Every block quantises the tokens for itself, its
+// warps shared out among them, while its first weights are on their way: one launch, no workspace.
+// 4096 -> 11008 takes 9.9 us, 11008 -> 4096 11.4, 7.0 of them for the bytes at a copy's rate and 1.7 for the launch.  With the loads in
+// registers, eight a lane, the issue slots showed (30 to 70 instructions a load): 12.4 and 15.5 us.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewThreads = 512, kFewWarps = kFewThreads / 32, kFewTokens = 2, kFewSegment = 4096, kFewSlots = 8;
+constexpr int kFewThreads = 512, kFewWarps = kFewThreads / 32, kFewTokens = 8, kFewSegment = 4096, kFewSlots = 8;
 constexpr int kFewSmem = 224 * 1024;
 __host__ __device__ constexpr int few_pitch(int k) { return (k + 511) / 512 * 512; }  // bytes of a token's codes: whole steps of 32 lanes
 
@@ -236,7 +239,7 @@ template <typename T, int M>
 __global__ void __launch_bounds__(kFewThreads, 1) linear_few_kernel(const __grid_constant__ LinearArgs a, const int slots, const int slot_bytes) {
   extern __shared__ __align__(16) uint8_t few_smem[];   // the warps' slots, then M rows of codes in whole steps, zero from the last whole 16 on
   __shared__ __align__(8) uint64_t full[kFewWarps][kFewSlots];
-  __shared__ uint32_t part[M][kFewWarps];
+  __shared__ uint32_t part[kFewWarps];
   __shared__ float sx[M];
   __shared__ int8_t rest[M][16];                        // the codes behind the last whole 16
   __shared__ int abort_flag;
@@ -273,57 +276,52 @@ __global__ void __launch_bounds__(kFewThreads, 1) linear_few_kernel(const __grid
   // the tokens' codes
   const T* x = static_cast<const T*>(a.x);
   const bool octets = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (M == 1 || a.m == 1 || (a.ldx * sizeof(T) & 15) == 0);
-  uint32_t amax[M];
-#pragma unroll
-  for (int m = 0; m < M; ++m) {
-    amax[m] = 0;
-    if (m < a.m) {
-      const T* src = x + m * a.ldx;
-      const int eights = octets ? a.k / 8 : 0;
+  constexpr int kShare = kFewWarps / M;                 // warps of a token
+  const int token = warp / kShare, at = (warp % kShare) * 32 + lane;
+  const T* src = x + token * a.ldx;
+  const bool exists = token < a.m;
+  uint32_t top = 0;
+  if (exists) {
+    const int eights = octets ? a.k / 8 : 0;
 #pragma unroll 4
-      for (int o = threadIdx.x; o < eights; o += kFewThreads) {
-        Octet<T> raw;
-        raw.load_shared(src + o * 8);
-        float v[8];
-        raw.unpack(v);
+    for (int o = at; o < eights; o += kShare * 32) {
+      Octet<T> raw;
+      raw.load_shared(src + o * 8);
+      float v[8];
+      raw.unpack(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) amax[m] = max(amax[m], magnitude(v[j]));
-      }
-#pragma unroll 4
-      for (int c = eights * 8 + threadIdx.x; c < a.k; c += kFewThreads) amax[m] = max(amax[m], magnitude(Storage<T>::load1(src + c)));
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[j]));
     }
-    amax[m] = __reduce_max_sync(0xFFFFFFFFu, amax[m]);
-    if (lane == 0) part[m][warp] = amax[m];
+#pragma unroll 4
+    for (int c = eights * 8 + at; c < a.k; c += kShare * 32) top = max(top, magnitude(Storage<T>::load1(src + c)));
   }
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  if (lane == 0) part[warp] = top;
   __syncthreads();
 #pragma unroll
-  for (int m = 0; m < M; ++m) {
-    uint32_t top = 0;
+  for (int i = 0; i < kShare; ++i) top = max(top, part[token * kShare + i]);
+  const RowScale rs = row_scale(top);
+  if (at == 0) sx[token] = rs.scale;
+  const bool some = exists && !rs.zero;
+  uint2* dst = reinterpret_cast<uint2*>(codes + token * steps * 32);
+#pragma unroll 2
+  for (int o = at; o < steps * 64; o += kShare * 32) {
+    uint2 q = make_uint2(0, 0);
+    if (some && o * 8 < whole) {
+      float v[8];
+      if (octets) {
+        Octet<T> raw;
+        raw.load_shared(src + o * 8);
+        raw.unpack(v);
+      } else {
 #pragma unroll
-    for (int i = 0; i < kFewWarps; ++i) top = max(top, part[m][i]);
-    const RowScale rs = row_scale(top);
-    if (threadIdx.x == 0) sx[m] = rs.scale;
-    const T* src = x + m * a.ldx;
-    const bool some = m < a.m && !rs.zero;
-    uint2* dst = reinterpret_cast<uint2*>(codes + m * steps * 32);
-    for (int o = threadIdx.x; o < steps * 64; o += kFewThreads) {
-      uint2 q = make_uint2(0, 0);
-      if (some && o * 8 < whole) {
-        float v[8];
-        if (octets) {
-          Octet<T> raw;
-          raw.load_shared(src + o * 8);
-          raw.unpack(v);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = Storage<T>::load1(src + o * 8 + j);
-        }
-        q = make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
+        for (int j = 0; j < 8; ++j) v[j] = Storage<T>::load1(src + o * 8 + j);
       }
-      dst[o] = q;
+      q = make_uint2(code4(v, rs.inv), code4(v + 4, rs.inv));
     }
-    if (threadIdx.x < 16) rest[m][threadIdx.x] = static_cast<int8_t>(some && whole + threadIdx.x < a.k ? code_of(Storage<T>::load1(src + whole + threadIdx.x), rs.inv) : 0);
+    dst[o] = q;
   }
+  if (at < 16) rest[token][at] = static_cast<int8_t>(some && whole + at < a.k ? code_of(Storage<T>::load1(src + whole + at), rs.inv) : 0);
   __syncthreads();
   bool ok = true;
   int slot = 0;
@@ -393,6 +391,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) linear_few_kernel(const __grid
 // way round the weights, which are read from memory once, fill the instruction's 128 rows whatever the number of tokens; a thread of the
 // epilogue has one channel (its scale and bias in registers) and a warp writes 32 neighbouring channels of a token at a time,
 // contiguous for every row length.
+// 8 tokens, 11008 -> 4096: 11.9 us and 1.3 for the quantiser in front, 7.0 of them for the weights; 64 tokens, 5120 -> 13824: 15.3 us, 11.
 // A tile's inner dimension is cut over a cluster of `split` CTAs when there are fewer tiles than multiprocessors.  Integer sums are exact in
 // any order; each CTA finishes a share of the tokens, the others write their part of it into slots of its shared memory (which no stage uses:
 // one barrier between the writes and the reads, and nobody has to stay for the others).
@@ -671,6 +670,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
 // of a tile runs beside the products of the next.
 // Barriers: full (of the even CTA) counts the bytes of both CTAs' copies; empty and acc_full are signalled in both CTAs by the even one's
 // commits; acc_empty (of the even CTA) counts the epilogue warps of both.
+// 8192 x 4096 -> 11008: 220 us, 3360 TOP/s, the tensor pipe 89 % active at the board's power cap.  Where k or the number of tokens is small,
+// operands from L2 bound it (about 65 bytes a cycle and multiprocessor): 1024 x 8192 -> 2048 takes 15.5 us, 10 at the rate above.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairStages = 6, kPairStageBytes = 2 * kTileChannels * kChunk;
 
@@ -1002,11 +1003,15 @@ FewShape few_shape(int64_t m, int64_t k) {
   const int row = std::max(512, few_pitch(static_cast<int>(k))), parts = (row + kFewSegment - 1) / kFewSegment;
   FewShape s = {0, few_pitch((row + parts - 1) / parts)};
   if (m > kFewTokens) return s;
-  const int64_t left = (kFewSmem - m * few_pitch(static_cast<int>(k))) / (kFewWarps * s.bytes);
+  const int held = m == 1 ? 1 : (m == 2 ? 2 : (m <= 4 ? 4 : 8));      // (the kernel's tokens)
+  const int64_t left = (kFewSmem - held * static_cast<int64_t>(few_pitch(static_cast<int>(k)))) / (kFewWarps * s.bytes);
   s.slots = left >= 2 ? static_cast<int>(std::min<int64_t>(left, kFewSlots)) : 0;
   return s;
 }
-bool few(int64_t m, int64_t k) { return few_shape(m, k).slots > 0; }
+// From three tokens on the tokens' codes are read from shared memory more often than the weights arrive, and the tile kernel is faster unless the
+// launch of the quantiser in front of it counts: 4 x 2048 -> 2048 4.6 us against 6.4, 4 x 4096 -> 4096 9.3 against 8.9, 8 x 4096 -> 1024 7.2
+// against 7.8, 8 x 4096 -> 4096 13.2 against 8.9; two tokens 4096 -> 11008 12.2 against 12.8.
+bool few(int64_t m, int64_t n, int64_t k) { return few_shape(m, k).slots > 0 && (m <= 2 || n * k <= (m <= 4 ? 1 << 23 : 1 << 22)); }
 template <typename T, int M>
 cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
@@ -1017,7 +1022,7 @@ cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
-  return a.m == 1 ? launch_few<T, 1>(a, st) : launch_few<T, kFewTokens>(a, st);
+  return a.m == 1 ? launch_few<T, 1>(a, st) : (a.m == 2 ? launch_few<T, 2>(a, st) : (a.m <= 4 ? launch_few<T, 4>(a, st) : launch_few<T, 8>(a, st)));
 }
 
 constexpr int64_t kMaxInner = 1 << 17;      // 127 * 127 * 2^17 < 2^31: the sums fit 32 bits
@@ -1071,9 +1076,9 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
   return run_quantize(dtype, x, ldx, rows, cols, codes, ldc, scales, 0, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
 
-int64_t zgr_linear_i8_workspace(int64_t m, int64_t k) {
-  if (m < 0 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF) return ZGR_EINVAL;
-  return few(m, k) ? 0 : scales_at(m, k) + m * static_cast<int64_t>(sizeof(float));
+int64_t zgr_linear_i8_workspace(int64_t m, int64_t n, int64_t k) {
+  if (m < 0 || n < 1 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF || n > 0x7FFFFFFF) return ZGR_EINVAL;
+  return few(m, n, k) ? 0 : scales_at(m, k) + m * static_cast<int64_t>(sizeof(float));
 }
 
 int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias, const void* residual, int64_t ldr, void* y,
@@ -1084,13 +1089,13 @@ int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, cons
   if (!matrix_ok(x, m, k, ldx, storage_size(dtype))) return ZGR_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
-  if (few(m, k)) {
+  if (few(m, n, k)) {
     a.x = x;
     a.ldx = ldx;
     const cudaError_t e = dtype == ZGR_F32 ? launch_few<float>(a, st) : (dtype == ZGR_F16 ? launch_few<__half>(a, st) : launch_few<__nv_bfloat16>(a, st));
     return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
   }
-  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_linear_i8_workspace(m, k)) return ZGR_EINVAL;
+  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_linear_i8_workspace(m, n, k)) return ZGR_EINVAL;
   int8_t* codes = static_cast<int8_t*>(workspace);
   float* scales = reinterpret_cast<float*>(codes + scales_at(m, k));
   if (run_quantize(dtype, x, ldx, m, k, codes, padded(k), scales, 1, st) != cudaSuccess) return ZGR_ECUDA;

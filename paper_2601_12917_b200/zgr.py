@@ -110,7 +110,7 @@ def lib() -> ctypes.CDLL:
         L.zgr_linear_status.argtypes = [ctypes.POINTER(i32)]
         for name in ("zgr_dropout", "zgr_dropout_backward", "zgr_quantize_rows", "zgr_linear_i8", "zgr_matmul_i8", "zgr_linear_status"):
             getattr(L, name).restype = ctypes.c_int
-        L.zgr_dropout_backward_workspace.argtypes = L.zgr_linear_i8_workspace.argtypes = [i64, i64]
+        L.zgr_dropout_backward_workspace.argtypes, L.zgr_linear_i8_workspace.argtypes = [i64, i64], [i64, i64, i64]
         L.zgr_dropout_backward_workspace.restype = L.zgr_linear_i8_workspace.restype = i64
         L.zgr_launch_count.argtypes = [vp]
         L.zgr_launch_count.restype = i64

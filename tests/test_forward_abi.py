@@ -46,11 +46,13 @@ def test_workspaces_cover_what_the_sizes_need():
         b = L.zgr_dropout_backward_workspace(rows, cols)
         assert b % (4 * cols) == 0 and 1 <= b // (4 * cols) <= 592           # one to four ranges for each of 148 multiprocessors
     assert L.zgr_dropout_backward_workspace(0, 8) == 0 and L.zgr_dropout_backward_workspace(-1, 8) == zgr.EINVAL
-    assert L.zgr_linear_i8_workspace(1, 4096) == 0
-    for m, k in ((5, 16), (100, 17), (8192, 4096), (4, 1 << 17)):
-        b = L.zgr_linear_i8_workspace(m, k)
+    for m, n, k in ((1, 11008, 4096), (2, 50265, 4096), (4, 2048, 4096), (8, 1024, 4096), (0, 8, 8)):      # quantised by the product itself
+        assert L.zgr_linear_i8_workspace(m, n, k) == 0
+    for m, n, k in ((9, 8, 16), (4, 4096, 4096), (8, 1025, 4096), (100, 50, 17), (8192, 4096, 4096), (1, 64, 1 << 17)):
+        b = L.zgr_linear_i8_workspace(m, n, k)
         assert b >= m * ((k + 15) // 16 * 16) + 4 * m
-    assert L.zgr_linear_i8_workspace(3, (1 << 17) + 1) == zgr.EINVAL and L.zgr_linear_i8_workspace(-1, 4) == zgr.EINVAL
+    for bad in ((3, 8, (1 << 17) + 1), (-1, 8, 4), (1, 0, 4), (1, 8, 0), (1, 1 << 31, 4)):
+        assert L.zgr_linear_i8_workspace(*bad) == zgr.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(c=None), dict(s=None), dict(s=A + 1), dict(ldx=7), dict(ldc=7), dict(cols=0), dict(rows=-1), dict(rows=1 << 31), dict(dtype=5), dict(x=A + 2)])
@@ -60,7 +62,7 @@ def test_quantize_refuses(kw):
     assert zgr.lib().zgr_quantize_rows(a["x"], a["ldx"], a["rows"], a["cols"], a["dtype"], a["c"], a["ldc"], a["s"], None) == zgr.EINVAL
 
 
-GOOD = dict(x=A, ldx=64, w=A, ldw=64, ws=A, bias=None, r=None, ldr=0, y=A, ldy=24, m=8, n=24, k=64, dtype=zgr.F32, p=0.0, space=A, space_bytes=1 << 20, xs=A)
+GOOD = dict(x=A, ldx=64, w=A, ldw=64, ws=A, bias=None, r=None, ldr=0, y=A, ldy=24, m=80, n=24, k=64, dtype=zgr.F32, p=0.0, space=A, space_bytes=1 << 20, xs=A)
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(w=A + 8), dict(ldw=72), dict(ldw=48), dict(ldx=63), dict(ldy=23), dict(r=A, ldr=20),
