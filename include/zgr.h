@@ -385,7 +385,7 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
  * qx, sx: the m x k tokens x quantised as by zgr_quantize_rows; w, w_scale: n x k codes and n scales, as zgr_quantize_rows makes them
  * of the weights (after a sweep: of the perturbed ones).  D is the dropout of zgr_dropout with cols = n (p = 0: nothing).
  * The sums are exact.  A token that holds an infinity or a NaN gives NaN in its row (where it is not dropped).
- * w: 16-byte aligned, ldw a multiple of 16 (what lies behind the k-th code of a row is not used).  k at most 2^17.  m may be 0.
+ * w: 16-byte aligned, ldw a multiple of 16, best of 128 (what lies behind the k-th code of a row is not used).  k at most 2^17.  m may be 0.
  * workspace: 16-byte aligned, at least zgr_linear_i8_workspace(m, n, k) bytes (0 for a few tokens, and it may be NULL then): the tokens'
  * codes and scales.  Its contents before the call do not matter.
  * ZGR_EINVAL: null or misaligned pointer, size out of range, ld below the row, unknown dtype, p outside [0, 1], workspace missing,

@@ -8,6 +8,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -135,10 +136,8 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t wanted, F&& body) {
     return c.code > 0 ? nullptr : PyLong_FromLong(c.code);      // (above 0: Python's own error is set)
   } catch (const Refused& e) {
     PyErr_SetString(PyExc_ValueError, e.what());
-  } catch (const c10::OutOfMemoryError& e) {
-    PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());      // torch's own, as its OutOfMemoryError
   }
   return nullptr;
 }
@@ -203,7 +202,8 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int storage = storage_of(x.scalar_type(), "x");
     if (x.dim() != 2) throw Refused("x must be a matrix");
     const Matrix m = matrix_of(x, "x");
-    int64_t pitch = (m.cols + 15) / 16 * 16;
+    const int64_t line = m.cols < 512 ? 16 : 128;
+    int64_t pitch = (m.cols + line - 1) / line * line;
     if (given(a[1])) {
       pitch = PyLong_AsLongLong(a[1]);
       if (pitch == -1 && PyErr_Occurred()) throw Code{1};

@@ -1041,7 +1041,8 @@ bool product_ok(const int8_t* w, int64_t ldw, const float* sw, const void* bias,
   if (!codes_ok(w, n, k, ldw) || !sw || !aligned_to(sw, 4) || !aligned_to(bias, size)) return false;
   return matrix_ok(y, m, n, ldy, size) && (!residual || matrix_ok(residual, m, n, ldr, size));
 }
-int64_t padded(int64_t k) { return (k + 15) / 16 * 16; }
+// Rows of the tokens' codes in the workspace: whole chunks, so that a box's rows are whole lines (at 16 bytes a box of 128 codes may touch two).
+int64_t padded(int64_t k) { return (k + kChunk - 1) / kChunk * kChunk; }
 int64_t scales_at(int64_t m, int64_t k) { return (m * padded(k) + 255) / 256 * 256; }
 
 LinearArgs linear_args(const int8_t* w, int64_t ldw, const float* sw, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m,

@@ -200,8 +200,8 @@ def dropout_backward(dy, p: float, seed: int, tensor: int = 0, bias_grad: bool =
 
 def quantize_rows(x, pitch: Optional[int] = None, stream=None):
     """Signed 8-bit codes of the rows of x (rows, cols) with a scale each (zgr_quantize_rows).  Returns (codes, scales); rows of codes
-    are `pitch` bytes apart, by default the next multiple of 16, which the products want; pitch = cols gives contiguous codes, which
-    set_coeffs_dtc wants."""
+    are `pitch` bytes apart, by default the next multiple of 128 (of 16 below 512 columns): the products want a multiple of 16 and are
+    faster where rows are whole lines; pitch = cols gives contiguous codes, which set_coeffs_dtc wants."""
     f = (_bind or _load_bind()).quantize_rows
     r = f(x, pitch) if stream is None else _on_stream(f, stream, x, pitch)
     if r.__class__ is int:

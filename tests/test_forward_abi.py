@@ -50,7 +50,7 @@ def test_workspaces_cover_what_the_sizes_need():
         assert L.zgr_linear_i8_workspace(m, n, k) == 0
     for m, n, k in ((9, 8, 16), (4, 4096, 4096), (8, 1025, 4096), (100, 50, 17), (8192, 4096, 4096), (1, 64, 1 << 17)):
         b = L.zgr_linear_i8_workspace(m, n, k)
-        assert b >= m * ((k + 15) // 16 * 16) + 4 * m
+        assert b >= m * ((k + 127) // 128 * 128) + 4 * m
     for bad in ((3, 8, (1 << 17) + 1), (-1, 8, 4), (1, 0, 4), (1, 8, 0), (1, 1 << 31, 4)):
         assert L.zgr_linear_i8_workspace(*bad) == zgr.EINVAL
 
