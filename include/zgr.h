@@ -365,7 +365,7 @@ int zgr_dropout(const void* x, int64_t ldx, const void* bias, const void* residu
 
 /* Its backward pass: dx = keep ? dy * s : 0 and, unless dbias is NULL, dbias = column sums of the unrounded dx, in fp32, added in an
  * order that depends on the sizes alone (repeated calls give identical bits).  The residual's gradient is dy itself.  dx may be dy.
- * workspace: 16-byte aligned, at least zgr_dropout_backward_workspace(rows, cols) bytes; not used (may be NULL) without dbias.  Its contents
+ * workspace: 16-byte aligned, at least zgr_dropout_backward_workspace(rows, cols) bytes; not used (may be NULL) without dbias or if that is 0.  Its contents
  * before the call do not matter.  rows = 0 writes zeros into dbias.
  * ZGR_EINVAL: as zgr_dropout; workspace missing, misaligned or too small. */
 int64_t zgr_dropout_backward_workspace(int64_t rows, int64_t cols);

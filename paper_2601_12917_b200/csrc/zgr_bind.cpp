@@ -179,10 +179,10 @@ PyObject* dropout_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (want) {
       db = empty({m.cols}, type, here);
       bytes = f_dropout_backward_workspace(m.rows, m.cols);
-      workspace = empty({bytes}, at::kByte, here);
+      if (bytes > 0) workspace = empty({bytes}, at::kByte, here);
     }
     check(f_dropout_backward(m.data, m.ld, dx.data, dx.ld, want ? db.data_ptr() : nullptr, m.rows, m.cols, storage, number(a[1]), bits64(a[2]),
-                             static_cast<uint32_t>(bits64(a[3])), want ? workspace.data_ptr() : nullptr, bytes, here.stream()));
+                             static_cast<uint32_t>(bits64(a[3])), bytes > 0 ? workspace.data_ptr() : nullptr, bytes, here.stream()));
     PyObject* out = given(a[5]) ? Py_NewRef(a[5]) : THPVariable_Wrap(made);
     if (!want || !out) return out;
     PyObject* grad = THPVariable_Wrap(db);

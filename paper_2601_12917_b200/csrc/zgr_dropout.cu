@@ -340,14 +340,14 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
 // 8192 x 2048 fp16: 12.5 us and 2.5 for the sums, 4.5 TB/s in all; bound by the generator's wide multiplies, which all warps issue at once
 // behind their loads, and by the ramp of the one wave of blocks.
 template <typename T, bool OCTETS, typename Index>
-__global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials) {
+__global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __grid_constant__ DropArgs<T> a, const int64_t rows_per_range, float* partials, T* direct) {
   __shared__ float sums[kThreads * 8];
   constexpr int kRowsInFlight = sizeof(T) == 2 ? 4 : 2;
   const int lane = threadIdx.x & 31, G = a.group, l = threadIdx.x & (G - 1);
   const int row_lane = threadIdx.x / G, row_lanes = kThreads / G;
   const int64_t o0 = static_cast<int64_t>(blockIdx.x) * G, c0 = o0 * 8;
   dependency_wait();
-  dependents_may_start();      // column_sums_kernel
+  if (direct == nullptr) dependents_may_start();      // column_sums_kernel
   const int64_t begin = static_cast<int64_t>(blockIdx.y) * rows_per_range, end = min(begin + rows_per_range, a.rows);
   const bool none = a.mask.threshold > 65535u;
   const uint32_t least = none ? 0xFFFFFFFFu : keep_least(a.mask);
@@ -435,7 +435,8 @@ __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __gr
     if (c0 + e < a.cols) {
       float t = 0.0f;
       for (int k = 0; k < row_lanes; ++k) t += sums[k * (8 * G) + e];
-      partials[blockIdx.y * a.cols + c0 + e] = t;
+      if (direct) Storage<T>::store1(direct + c0 + e, t);      // one range: these are the sums
+      else partials[blockIdx.y * a.cols + c0 + e] = t;
     }
   }
 }
@@ -465,8 +466,8 @@ int group_for(int64_t octets) {
   return g;
 }
 
-// How the rows of a backward pass with column sums are cut: enough ranges for four blocks on each of the 148 multiprocessors, each of
-// at least four rows a thread.  A function of the sizes alone, so that the sums do not depend on the device.
+// How the rows of a backward pass with column sums are cut: one range, whose sums need no second kernel, up to sixteen rows a thread; else
+// enough ranges for four blocks on each of the 148 multiprocessors, each of at least four rows a thread.  A function of the sizes alone, so that the sums do not depend on the device.
 struct Ranges {
   int64_t count, rows;
 };
@@ -474,7 +475,7 @@ Ranges cut_ranges(int64_t rows, int64_t cols) {
   const int64_t octets = (cols + 7) / 8;
   const int g = group_for(octets);
   const int64_t strips = (octets + g - 1) / g, trip = static_cast<int64_t>(kThreads / g) * 4;
-  const int64_t want = std::max<int64_t>(1, 592 / strips), trips = (rows + trip - 1) / trip;
+  const int64_t trips = (rows + trip - 1) / trip, want = trips <= 4 ? 1 : std::max<int64_t>(1, 592 / strips);
   Ranges r;
   const int64_t even = (rows + std::min(want, trips) - 1) / std::min(want, trips), lanes = kThreads / g;
   r.rows = (even + lanes - 1) / lanes * lanes;
@@ -535,8 +536,8 @@ int run_backward_bias(DropArgs<T> a, T* dbias, float* partials, cudaStream_t st)
   const bool far = a.rows * a.octets >= int64_t{1} << 32;      // block numbers of 64 bits
   const auto kernel = far ? (octets ? dropout_columns_kernel<T, true, uint64_t> : dropout_columns_kernel<T, false, uint64_t>)
                           : (octets ? dropout_columns_kernel<T, true, uint32_t> : dropout_columns_kernel<T, false, uint32_t>);
-  if (launch_behind(kernel, grid, kThreads, 0, 1, st, a, r.rows, partials) != cudaSuccess)
-    return ZGR_ECUDA;
+  if (launch_behind(kernel, grid, kThreads, 0, 1, st, a, r.rows, partials, r.count == 1 ? dbias : nullptr) != cudaSuccess) return ZGR_ECUDA;
+  if (r.count == 1) return ZGR_OK;
   const cudaError_t e = launch_behind(column_sums_kernel<T>, static_cast<unsigned>((a.cols + 31) / 32), dim3(32, 8), 0, 1, st, partials, static_cast<int>(r.count), a.cols, dbias);
   return e == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
 }
@@ -585,7 +586,8 @@ int zgr_dropout(const void* x, int64_t ldx, const void* bias, const void* residu
 int64_t zgr_dropout_backward_workspace(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0) return ZGR_EINVAL;
   if (rows == 0 || cols == 0) return 0;
-  return cut_ranges(rows, cols).count * cols * static_cast<int64_t>(sizeof(float));
+  const int64_t ranges = cut_ranges(rows, cols).count;
+  return ranges == 1 ? 0 : ranges * cols * static_cast<int64_t>(sizeof(float));
 }
 
 int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dbias, int64_t rows, int64_t cols, int32_t dtype, double p,
@@ -599,7 +601,8 @@ int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, v
     return !dbias || cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * size, st) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;
   if (!matrix_ok(dy, rows, cols, lddy, size) || !matrix_ok(dx, rows, cols, lddx, size)) return ZGR_EINVAL;
   if (!dbias) return zgr_dropout(dy, lddy, nullptr, nullptr, 0, dx, lddx, rows, cols, dtype, p, seed, tensor, stream);
-  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < zgr_dropout_backward_workspace(rows, cols)) return ZGR_EINVAL;
+  const int64_t need = zgr_dropout_backward_workspace(rows, cols);
+  if (need > 0 && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return ZGR_EINVAL;
   const DropMask mask = make_drop_mask(p, seed, tensor);
   float* partials = static_cast<float*>(workspace);
   switch (dtype) {

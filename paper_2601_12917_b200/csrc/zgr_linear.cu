@@ -1010,8 +1010,11 @@ FewShape few_shape(int64_t m, int64_t k) {
 }
 // From three tokens on the tokens' codes are read from shared memory more often than the weights arrive, and the tile kernel is faster unless the
 // launch of the quantiser in front of it counts: 4 x 2048 -> 2048 4.6 us against 6.4, 4 x 4096 -> 4096 9.3 against 8.9, 8 x 4096 -> 1024 7.2
-// against 7.8, 8 x 4096 -> 4096 13.2 against 8.9; two tokens 4096 -> 11008 12.2 against 12.8.
-bool few(int64_t m, int64_t n, int64_t k) { return few_shape(m, k).slots > 0 && (m <= 2 || n * k <= (m <= 4 ? 1 << 23 : 1 << 22)); }
+// against 7.8, 8 x 4096 -> 4096 13.2 against 8.9; two tokens 4096 -> 11008 12.2 against 12.8.  A channel costs a warp the same however short
+// its row is: 4 x 19 -> 22047 12.4 against 8.2.
+bool few(int64_t m, int64_t n, int64_t k) {
+  return few_shape(m, k).slots > 0 && (m <= 2 || (n <= 8192 && n * k <= (m <= 4 ? 1 << 23 : 1 << 22)));
+}
 template <typename T, int M>
 cudaError_t launch_few(const LinearArgs& a, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);

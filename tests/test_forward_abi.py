@@ -29,7 +29,7 @@ def test_nothing_to_do_is_not_an_error():
     assert L.zgr_linear_i8(None, 0, None, 0, None, None, None, 0, None, 0, 0, 5, 7, zgr.F32, 0.0, 0, 0, None, 0, None) == zgr.OK
 
 
-def back(dy=A, dx=A, db=A, rows=100, cols=64, ws=A, ws_bytes=None, dtype=zgr.F32, p=0.1):
+def back(dy=A, dx=A, db=A, rows=10000, cols=64, ws=A, ws_bytes=None, dtype=zgr.F32, p=0.1):
     L = zgr.lib()
     need = L.zgr_dropout_backward_workspace(rows, cols)
     return L.zgr_dropout_backward(dy, cols, dx, cols, db, rows, cols, dtype, p, 1, 0, ws, need if ws_bytes is None else need + ws_bytes, None)
@@ -42,13 +42,15 @@ def test_dropout_backward_refuses(kw):
 
 def test_workspaces_cover_what_the_sizes_need():
     L = zgr.lib()
-    for rows, cols in ((1, 1), (1, 100000), (7, 5), (4096, 1024), (1 << 20, 8), (100000, 300)):
+    for rows, cols in ((4096, 1024), (1 << 20, 8), (100000, 300), (129, 1000), (4097, 1)):
         b = L.zgr_dropout_backward_workspace(rows, cols)
-        assert b % (4 * cols) == 0 and 1 <= b // (4 * cols) <= 592           # one to four ranges for each of 148 multiprocessors
+        assert b % (4 * cols) == 0 and 2 <= b // (4 * cols) <= 592           # up to four ranges for each of 148 multiprocessors
+    for rows, cols in ((1, 1), (1, 100000), (7, 5), (128, 1000), (4096, 1), (200, 128)):
+        assert L.zgr_dropout_backward_workspace(rows, cols) == 0             # one range: its sums are the result
     assert L.zgr_dropout_backward_workspace(0, 8) == 0 and L.zgr_dropout_backward_workspace(-1, 8) == zgr.EINVAL
     for m, n, k in ((1, 11008, 4096), (2, 50265, 4096), (4, 2048, 4096), (8, 1024, 4096), (0, 8, 8)):      # quantised by the product itself
         assert L.zgr_linear_i8_workspace(m, n, k) == 0
-    for m, n, k in ((9, 8, 16), (4, 4096, 4096), (8, 1025, 4096), (100, 50, 17), (8192, 4096, 4096), (1, 64, 1 << 17)):
+    for m, n, k in ((9, 8, 16), (4, 8193, 16), (4, 4096, 4096), (8, 1025, 4096), (100, 50, 17), (8192, 4096, 4096), (1, 64, 1 << 17)):
         b = L.zgr_linear_i8_workspace(m, n, k)
         assert b >= m * ((k + 127) // 128 * 128) + 4 * m
     for bad in ((3, 8, (1 << 17) + 1), (-1, 8, 4), (1, 0, 4), (1, 8, 0), (1, 1 << 31, 4)):

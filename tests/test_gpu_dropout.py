@@ -12,8 +12,9 @@ from paper_2601_12917_b200 import zgr
 pytestmark = pytest.mark.gpu
 DT = ref.DTYPES
 # one element to several octets, ends of octets, rows of 1, 8, 32 and more octets, several blocks of 256 threads, the line between the
-# one-octet and the four-octet form (148 * 8 * 256 octets)
-SHAPES = [(1, 1), (1, 7), (3, 8), (5, 9), (2, 256), (7, 255), (33, 40), (4, 1000), (3, 4096), (130, 129), (1, 70001), (2371, 1024), (600, 4100)]
+# one-octet and the four-octet form (148 * 8 * 256 octets), column sums by one range of rows and by several
+SHAPES = [(1, 1), (1, 7), (3, 8), (5, 9), (2, 256), (7, 255), (33, 40), (4, 1000), (3, 4096), (130, 129), (1, 70001), (2371, 1024), (600, 4100),
+          (128, 300), (129, 300), (4096, 3), (4097, 3), (300, 64), (1100, 24), (513, 63)]
 
 
 def make(shape, dtype, seed=0, sigma=1.0):

@@ -90,7 +90,7 @@ def run_case(m, k, n, dtype, p, bias, residual, seed=0):
                                    (31, 1024, 100), (33, 2048, 64), (64, 4096, 130), (100, 1000, 300), (128, 384, 256), (129, 512, 640), (255, 136, 65),
                                    (256, 256, 256), (257, 300, 384), (300, 1027, 200), (520, 2050, 140), (1, 4096, 1000), (8, 11008, 520), (4, 24000, 64), (4, 24600, 64), (2000, 300, 2500), (1030, 1100, 2100), (3, 6000, 9000), (16, 6145, 20000),
                                    (15, 12200, 5000), (16, 16000, 6000), (13, 1000, 19000),
-                                   (3, 4100, 2048), (3, 4100, 2040), (5, 4100, 1024), (8, 4100, 1020), (6, 300, 700), (8, 11000, 300), (7, 31, 50)])
+                                   (3, 4100, 2048), (3, 4100, 2040), (5, 4100, 1024), (8, 4100, 1020), (6, 300, 700), (8, 11000, 300), (7, 31, 50), (4, 40, 8192), (5, 40, 8193)])
 @pytest.mark.parametrize("dtype", list(DT))
 def test_linear_sizes(m, k, n, dtype):
     run_case(m, k, n, dtype, 0.0, n % 2 == 0, m % 2 == 0)
