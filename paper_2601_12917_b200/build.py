@@ -50,7 +50,7 @@ def _build_bind() -> None:
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=1",
                     "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                     "-isystem", os.path.join(cuda, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(_ROOT, "include"),
-                    os.path.join(CSRC, BIND_SOURCE), "-o", tmp, "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"],
+                    os.path.join(CSRC, BIND_SOURCE), "-o", tmp, "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"],
                    check=True)
     os.replace(tmp, BIND)
 
