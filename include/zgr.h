@@ -346,7 +346,8 @@ int64_t zgr_launch_count(const zgr_ctx* ctx);
  * pointers are device pointers of the current device, the work is enqueued on `stream`, and the calls are safe from several threads.  Matrices
  * are row-major with rows `ld` elements apart (ld >= columns; any alignment of the element size), of one storage type `dtype`
  * (ZGR_F32, ZGR_F16, ZGR_BF16) for all matrices and vectors of a call.  Arithmetic in fp32, one rounding to the storage type.  An output may be
- * the very matrix of an input of the same shape (same address, same ld); other overlaps are not allowed.  A call
+ * the very matrix of an input that is added to it or masked into it (same address, same ld): x or residual of zgr_dropout, dy of its backward
+ * pass, residual of the products; other overlaps are not allowed, the tokens of a product among them.  A call
  * recorded into a graph repeats its seed on every replay.  No call allocates, and calls that may run at the same time need workspaces of
  * their own.
  * ------------------------------------------------------------------------------------------------------------ */
@@ -388,8 +389,8 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
  * w: 16-byte aligned, ldw a multiple of 16, best of 128 (what lies behind the k-th code of a row is not used).  k at most 2^17.  m may be 0.
  * workspace: 16-byte aligned, at least zgr_linear_i8_workspace(m, n, k) bytes (0 for a few tokens, and it may be NULL then): the tokens'
  * codes and scales.  Its contents before the call do not matter.
- * ZGR_EINVAL: null or misaligned pointer, size out of range, ld below the row, unknown dtype, p outside [0, 1], workspace missing,
- * misaligned or too small. */
+ * ZGR_EINVAL: null or misaligned pointer, size out of range, ld below the row, unknown dtype, p outside [0, 1], y the same address as x,
+ * workspace missing, misaligned or too small. */
 int64_t zgr_linear_i8_workspace(int64_t m, int64_t n, int64_t k);
 int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias, const void* residual, int64_t ldr, void* y,
                   int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed, uint32_t tensor, void* workspace,

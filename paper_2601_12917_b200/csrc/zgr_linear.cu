@@ -1090,7 +1090,7 @@ int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, cons
                   int64_t workspace_bytes, void* stream) {
   if (!product_ok(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p)) return ZGR_EINVAL;
   if (m == 0) return ZGR_OK;
-  if (!matrix_ok(x, m, k, ldx, storage_size(dtype))) return ZGR_EINVAL;
+  if (!matrix_ok(x, m, k, ldx, storage_size(dtype)) || x == y) return ZGR_EINVAL;      // (blocks read all of x while others write results)
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
   if (few(m, n, k)) {
@@ -1112,7 +1112,7 @@ int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8
                   uint32_t tensor, void* stream) {
   if (!product_ok(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p)) return ZGR_EINVAL;
   if (m == 0) return ZGR_OK;
-  if (!codes_ok(x, m, k, ldx) || !x_scale || !aligned_to(x_scale, 4)) return ZGR_EINVAL;
+  if (!codes_ok(x, m, k, ldx) || !x_scale || !aligned_to(x_scale, 4) || static_cast<const void*>(x) == y) return ZGR_EINVAL;
   LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
   a.sx = x_scale;
   return run_product(x, ldx, a, dtype, false, static_cast<cudaStream_t>(stream));

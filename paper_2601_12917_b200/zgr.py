@@ -211,7 +211,8 @@ def quantize_rows(x, pitch: Optional[int] = None, stream=None):
 
 def linear_i8(x, w, w_scale, bias=None, residual=None, p: float = 0.0, seed: int = 0, tensor: int = 0, out=None, stream=None):
     """residual + dropout(x w^T + bias) in 8 bits (zgr_linear_i8): x (..., k) is quantised with a scale for each token, w (n, k) and
-    w_scale (n) are the codes and scales that quantize_rows makes of the weights.  Returns (..., n) of x's type."""
+    w_scale (n) are the codes and scales that quantize_rows makes of the weights.  Returns (..., n) of x's type; out may be the residual
+    itself, not x."""
     f = (_bind or _load_bind()).linear_i8
     r = (f(x, w, w_scale, bias, residual, p, seed, tensor, out) if stream is None
          else _on_stream(f, stream, x, w, w_scale, bias, residual, p, seed, tensor, out))

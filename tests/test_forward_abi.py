@@ -64,7 +64,7 @@ def test_quantize_refuses(kw):
     assert zgr.lib().zgr_quantize_rows(a["x"], a["ldx"], a["rows"], a["cols"], a["dtype"], a["c"], a["ldc"], a["s"], None) == zgr.EINVAL
 
 
-GOOD = dict(x=A, ldx=64, w=A, ldw=64, ws=A, bias=None, r=None, ldr=0, y=A, ldy=24, m=80, n=24, k=64, dtype=zgr.F32, p=0.0, space=A, space_bytes=1 << 20, xs=A)
+GOOD = dict(x=A, ldx=64, w=A, ldw=64, ws=A, bias=None, r=None, ldr=0, y=A + (1 << 20), ldy=24, m=80, n=24, k=64, dtype=zgr.F32, p=0.0, space=A, space_bytes=1 << 20, xs=A)
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(w=A + 8), dict(ldw=72), dict(ldw=48), dict(ldx=63), dict(ldy=23), dict(r=A, ldr=20),
@@ -75,6 +75,14 @@ def test_linear_refuses(kw):
     rc = zgr.lib().zgr_linear_i8(a["x"], a["ldx"], a["w"], a["ldw"], a["ws"], a["bias"], a["r"], a["ldr"], a["y"], a["ldy"], a["m"], a["n"], a["k"], a["dtype"], a["p"], 0, 0,
                                  a["space"], a["space_bytes"], None)
     assert rc == zgr.EINVAL
+
+
+@pytest.mark.parametrize("m", [1, 4, 80])
+def test_a_product_refuses_its_tokens_as_the_output(m):
+    # for a few tokens every block reads all of them while others write: the order would decide what it reads
+    L, X = zgr.lib(), A + (1 << 20)
+    assert L.zgr_linear_i8(X, 64, A, 64, A, None, X, 64, X, 64, m, 64, 64, zgr.F32, 0.0, 0, 0, A, 1 << 20, None) == zgr.EINVAL
+    assert L.zgr_matmul_i8(X, 64, A, A, 64, A, None, None, 0, X, 64, m, 64, 64, zgr.F32, 0.0, 0, 0, None) == zgr.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(x=None), dict(xs=None), dict(xs=A + 2), dict(x=A + 8), dict(ldx=72), dict(ldx=1 << 40), dict(w=None), dict(k=0), dict(p=3.0)])
