@@ -584,7 +584,7 @@ int zgr_dropout(const void* x, int64_t ldx, const void* bias, const void* residu
 }
 
 int64_t zgr_dropout_backward_workspace(int64_t rows, int64_t cols) {
-  if (rows < 0 || cols < 0) return ZGR_EINVAL;
+  if (rows < 0 || cols < 0 || (cols > 0 && rows > kMostElements / cols)) return ZGR_EINVAL;
   if (rows == 0 || cols == 0) return 0;
   const int64_t ranges = cut_ranges(rows, cols).count;
   return ranges == 1 ? 0 : ranges * cols * static_cast<int64_t>(sizeof(float));
@@ -595,7 +595,7 @@ int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, v
   if (!storage_known(dtype) || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return ZGR_EINVAL;
   const int size = storage_size(dtype);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (dbias && !aligned_to(dbias, size)) return ZGR_EINVAL;
+  if ((dbias && !aligned_to(dbias, size)) || cols > kMostElements) return ZGR_EINVAL;
   if (cols == 0) return ZGR_OK;
   if (rows == 0)      // no rows: the sums are zero
     return !dbias || cudaMemsetAsync(dbias, 0, static_cast<size_t>(cols) * size, st) == cudaSuccess ? ZGR_OK : ZGR_ECUDA;

@@ -186,11 +186,12 @@ cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size
 inline int storage_size(int32_t dtype) { return dtype == 0 ? 4 : 2; }
 inline bool storage_known(int32_t dtype) { return dtype >= 0 && dtype <= 2; }
 inline bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0; }
+constexpr int64_t kMostElements = int64_t{1} << 60;      // of a row, and of `ld` times the rows: no sum of sizes passes 63 bits
 // A rows x cols matrix of the storage type with rows `ld` elements apart: no row reaches into the next, offsets stay below 2^62 bytes.
 inline bool matrix_ok(const void* p, int64_t rows, int64_t cols, int64_t ld, int size) {
   if (!p || !aligned_to(p, size)) return false;
   if (rows > 1 && ld < cols) return false;
-  return ld >= 0 && (rows == 0 || ld <= (int64_t{1} << 60) / rows);
+  return ld >= 0 && cols <= kMostElements && (rows == 0 || ld <= kMostElements / rows);
 }
 // Elements between a 16-byte boundary and the row; all rows of a matrix have the same if `ld` is a whole number of 16 bytes.
 inline int phase_of(const void* p, int size) { return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / size); }

@@ -40,6 +40,16 @@ def test_dropout_backward_refuses(kw):
     assert back(**kw) == zgr.EINVAL
 
 
+def test_sizes_whose_sums_would_pass_63_bits_are_refused():
+    L, huge = zgr.lib(), (1 << 63) - 1
+    assert drop(rows=1, cols=huge, ldx=0, ldy=0) == zgr.EINVAL and drop(rows=huge, cols=1, ldx=1, ldy=1) == zgr.EINVAL
+    for rows, cols in ((1, huge), (huge, 1), (huge, huge)):
+        assert L.zgr_dropout_backward_workspace(rows, cols) == zgr.EINVAL
+        assert L.zgr_dropout_backward(A, cols, A, cols, A, rows, cols, zgr.F32, 0.5, 1, 0, A, huge, None) == zgr.EINVAL
+    assert L.zgr_dropout_backward(A, 0, A, 0, A, 0, huge, zgr.F32, 0.5, 1, 0, A, huge, None) == zgr.EINVAL
+    assert L.zgr_quantize_rows(A, 0, 1, huge, zgr.F32, A, 0, A, None) == zgr.EINVAL
+
+
 def test_workspaces_cover_what_the_sizes_need():
     L = zgr.lib()
     for rows, cols in ((4096, 1024), (1 << 20, 8), (100000, 300), (129, 1000), (4097, 1)):
