@@ -49,6 +49,7 @@ struct Here {
   void check(const at::Tensor& t, const char* what) const {
     if (!t.is_cuda() || t.get_device() != device) throw Refused(std::string(what) + " must be on the current CUDA device");
     if (t.layout() != at::kStrided) throw Refused(std::string(what) + " must be a dense tensor");
+    if (t.is_neg()) throw Refused(std::string(what) + " must not be a view whose sign is still to be changed (resolve_neg)");
   }
   void* stream() const { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream(); }
 };
@@ -123,6 +124,13 @@ struct Workspace {
   Workspace& operator=(const Workspace&) = delete;
 };
 
+// The caller's output: written behind torch's back, so its version says it, and autograd refuses a saved tensor that is no longer itself.
+PyObject* written(PyObject* o) {
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  return Py_NewRef(o);
+}
+
 double number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Code{1};
@@ -172,7 +180,7 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Matrix y = given(a[6]) ? same(here, a[6], "out", type, x.sizes()) : matrix_of(made, "out");
     check(f_dropout(m.data, m.ld, bias, r.data, r.ld, y.data, y.ld, m.rows, m.cols, storage, number(a[1]), bits64(a[2]), static_cast<uint32_t>(bits64(a[3])),
                     here.stream()));
-    return given(a[6]) ? Py_NewRef(a[6]) : THPVariable_Wrap(made);
+    return given(a[6]) ? written(a[6]) : THPVariable_Wrap(made);
   });
 }
 
@@ -194,7 +202,7 @@ PyObject* dropout_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Workspace workspace(bytes, here.stream());
     check(f_dropout_backward(m.data, m.ld, dx.data, dx.ld, want ? db.data_ptr() : nullptr, m.rows, m.cols, storage, number(a[1]), bits64(a[2]),
                              static_cast<uint32_t>(bits64(a[3])), workspace.data, bytes, here.stream()));
-    PyObject* out = given(a[5]) ? Py_NewRef(a[5]) : THPVariable_Wrap(made);
+    PyObject* out = given(a[5]) ? written(a[5]) : THPVariable_Wrap(made);
     if (!want || !out) return out;
     PyObject* grad = THPVariable_Wrap(db);
     PyObject* both = grad ? PyTuple_Pack(2, out, grad) : nullptr;
@@ -275,7 +283,7 @@ PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Workspace workspace(bytes, here.stream());
     check(f_linear_i8(m.data, m.ld, static_cast<const int8_t*>(p.w.data), p.w.ld, p.w_scale, p.bias, p.residual.data, p.residual.ld, p.y.data, p.y.ld, m.rows, p.w.rows,
                       m.cols, storage, p.p, p.seed, p.tensor, workspace.data, bytes > 0 ? bytes : 0, here.stream()));
-    return given(a[8]) ? Py_NewRef(a[8]) : THPVariable_Wrap(p.made);
+    return given(a[8]) ? written(a[8]) : THPVariable_Wrap(p.made);
   });
 }
 
@@ -292,7 +300,7 @@ PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Product p = product_of(here, a + 3, type, THPVariable_Unpack(a[0]), m.cols);
     check(f_matmul_i8(static_cast<const int8_t*>(m.data), m.ld, x_scale, static_cast<const int8_t*>(p.w.data), p.w.ld, p.w_scale, p.bias, p.residual.data, p.residual.ld,
                       p.y.data, p.y.ld, m.rows, p.w.rows, m.cols, static_cast<int32_t>(storage), p.p, p.seed, p.tensor, here.stream()));
-    return given(a[10]) ? Py_NewRef(a[10]) : THPVariable_Wrap(p.made);
+    return given(a[10]) ? written(a[10]) : THPVariable_Wrap(p.made);
   });
 }
 

@@ -248,3 +248,22 @@ def test_calls_from_several_threads():
         t.join()
     for w, ys in zip(want, got):
         assert len(ys) == 50 and all(torch.equal(w, y) for y in ys)
+
+
+def test_outputs_count_as_written_and_pending_signs_are_refused():
+    x = make((6, 16), "f32").requires_grad_()
+    y = (x * x).sum()
+    zgr.dropout(x.detach(), 0.5, 1)
+    zgr.dropout_backward(x.detach(), 0.5, 1)
+    y.backward(retain_graph=True)
+    for write in (lambda: zgr.dropout(x.detach(), 0.5, 1, out=x.detach()), lambda: zgr.dropout_backward(x.detach(), 0.5, 1, out=x.detach())):
+        y = (x * x).sum()
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    with torch.inference_mode():
+        z = make((6, 16), "f32")
+        assert zgr.dropout(z, 0.5, 1, out=z) is z
+    assert zgr.dropout(z, 0.5, 1, out=z) is z
+    with pytest.raises(ValueError):
+        zgr.dropout(x.detach()._neg_view(), 0.5, 1)
