@@ -904,8 +904,14 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(rows > 1 ? pitch : (k + 15) / 16 * 16)};
   const cuuint32_t box[2] = {kChunk, static_cast<cuuint32_t>(box_rows)};
   const cuuint32_t ones[2] = {1, 1};
-  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  auto encode = [&] {
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (encode()) return true;
+  // A thread that has made no call of the runtime yet may have no context, which this call of the driver does not make for it.
+  int device;
+  return cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encode();
 }
 
 // Kernel, tokens per tile and CTAs per tile: the choice with the shortest estimate, in cycles of a multiprocessor.  From sweeps of all choices

@@ -1,5 +1,7 @@
 """Row quantiser and 8-bit linear layer against the 64-bit form: sizes around tiles, chunks and codes' ends, every epilogue, layouts,
 values that are not finite, graphs, refusals, and the run of them with a sweep between."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -284,3 +286,22 @@ def test_rows_behind_each_other_at_large_offsets():
     for row in (0, 30000, 61500, m - 1):
         assert torch.equal(y[row], small[row % 128])
     assert zgr.linear_status() == 0
+
+
+def test_a_new_thread_may_begin_with_a_product_of_codes():
+    # its first call of the driver is the description of the operands, which wants a context
+    xq, xs = zgr.quantize_rows(make((48, 256), "bf16"))
+    wq, ws = zgr.quantize_rows(make((200, 256), "bf16", 1))
+    want, out, got = zgr.matmul_i8(xq, xs, wq, ws), torch.empty((48, 200), dtype=torch.bfloat16, device="cuda"), []
+    torch.cuda.synchronize()
+
+    def work():
+        try:
+            got.append(zgr.matmul_i8(xq, xs, wq, ws, out=out))
+        except Exception as e:
+            got.append(e)
+    t = threading.Thread(target=work)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert got[0] is out and torch.equal(out, want)
