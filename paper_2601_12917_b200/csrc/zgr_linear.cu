@@ -470,7 +470,7 @@ __device__ __forceinline__ void load_scales(const LinearArgs& a, int64_t m0, int
   __syncwarp();
 }
 
-template <typename T, bool DROP, int U>
+template <typename T, bool DROP, bool RES, int U>
 __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum)[U], const float* sx, int64_t m0, int64_t n, float sw, float bias,
                                        const T (&add)[U]) {
   const int lane = threadIdx.x & 31;
@@ -482,7 +482,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum
 #pragma unroll
   for (int j = 0; j < U; ++j) {
     const uint32_t bits = DROP ? __shfl_sync(0xFFFFFFFFu, keep[j / 8], (lane & 24) | (j & 7)) : 0u;
-    v[j] = finish1(static_cast<int>(sum[j]), sx[j], sw, bias, a.residual ? Storage<T>::load1(add + j) : 0.0f, bits >> (lane & 7) & 1, a.mask.scale, DROP);
+    v[j] = finish1(static_cast<int>(sum[j]), sx[j], sw, bias, RES ? Storage<T>::load1(add + j) : 0.0f, bits >> (lane & 7) & 1, a.mask.scale, DROP);
   }
   if (n < a.n) {
     T* y = static_cast<T*>(a.y) + m0 * a.ldy + n;
@@ -498,7 +498,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum
   }
 }
 
-template <typename T, bool DROP>
+template <typename T, bool DROP, bool RES>
 __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                                    const LinearArgs a, const TileShape shape) {
   extern __shared__ uint8_t tile_smem[];
@@ -601,7 +601,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
       if (a.bias) bias = load_one<T>(a.bias, n);
     }
     T add[16];
-    if (shape.split == 1 && a.residual) residual_ahead<T, 16>(a, m0 + half * 16, n, add);
+    if (RES && shape.split == 1) residual_ahead<T, 16>(a, m0 + half * 16, n, add);
     ok = mbar_wait<false>(smem_u32(&done), 0, aborted, &g_linear_error, 103);
     ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
     ok = __all_sync(0xFFFFFFFFu, ok);
@@ -611,10 +611,10 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         uint32_t v[16];
         T next[16];
         tmem_ld16(mine + c, v);
-        if (a.residual && c + 32 < shape.tokens) residual_ahead<T, 16>(a, m0 + c + 32, n, next);
+        if (RES && c + 32 < shape.tokens) residual_ahead<T, 16>(a, m0 + c + 32, n, next);
         tmem_ld_wait();
-        finish<T, DROP, 16>(a, v, scales[warp - 2] + c / 32 * 16, m0 + c, n, sw, bias, add);
-        if (a.residual) {
+        finish<T, DROP, RES, 16>(a, v, scales[warp - 2] + c / 32 * 16, m0 + c, n, sw, bias, add);
+        if (RES) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) add[j] = next[j];
         }
@@ -644,14 +644,14 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         const int g = ((place >> 1) * shape.split + static_cast<int>(rank)) * 2 + (place & 1);
         if (g >= groups || m0 + g * 8 >= a.m) break;
         T add[8];
-        if (a.residual) residual_ahead<T, 8>(a, m0 + g * 8, n, add);
+        if (RES) residual_ahead<T, 8>(a, m0 + g * 8, n, add);
         float sx[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sx[j] = a.sx[min(m0 + g * 8 + j, a.m - 1)];
         uint32_t sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = sum_of_slots(sums0 + (place * 8 + j) * kTileChannels * 4 + channel, slot_bytes, shape.split);
-        finish<T, DROP, 8>(a, sum, sx, m0 + g * 8, n, sw, bias, add);
+        finish<T, DROP, RES, 8>(a, sum, sx, m0 + g * 8, n, sw, bias, add);
       }
     }
   }
@@ -707,7 +707,7 @@ __device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
 // the registers do not reach.  An accumulator is given back as soon as its last columns are in registers, with a release within the CTA: one for the cluster
 // made the warp wait for its stores.
 constexpr int kPairEpilogue = 12, kPairThreads = 64 + kPairEpilogue * 32, kPairStep = kPairEpilogue / 4 * 16;
-template <typename T, bool DROP>
+template <typename T, bool DROP, bool RES>
 __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                                    const LinearArgs a, const TileShape shape, const int64_t tiles) {
   extern __shared__ uint8_t pair_smem[];
@@ -721,6 +721,18 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
   const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int chunks = (a.k + kChunk - 1) / kChunk;
   const int half_tokens = shape.tokens / 2;
+  // a pair's tiles, `pairs` apart: counted on instead of divided (a 64-bit division takes longer than a short tile's products)
+  const int step_n = static_cast<int>(pairs / shape.token_tiles), step_m = static_cast<int>(pairs % shape.token_tiles);
+  const int first_n = static_cast<int>(pair / shape.token_tiles), first_m = static_cast<int>(pair % shape.token_tiles);
+  struct Place {
+    int n, m;            // tiles of channels and of tokens
+  };
+  auto behind = [&](Place p) {
+    p.n += step_n;
+    p.m += step_m;
+    if (p.m >= shape.token_tiles) p.m -= shape.token_tiles, ++p.n;
+    return p;
+  };
   volatile int* aborted = &abort_flag;
   if (threadIdx.x == 0) {
     prefetch_map(map_w);
@@ -753,12 +765,13 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
       const int ahead = shape.weights_ahead ? min(kPairStages, chunks) : 0, stage_bytes = (kTileChannels + half_tokens) * kChunk;
       for (int s = 0; s < ahead; ++s) {
         if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * stage_bytes);
-        tma_load_pair(stages0 + s * kPairStageBytes, &map_w, s * kChunk, static_cast<int>(pair / shape.token_tiles * 256 + rank * 128), peer_smem(smem_u32(&full[s]), 0));
+        tma_load_pair(stages0 + s * kPairStageBytes, &map_w, s * kChunk, static_cast<int>(first_n * 256 + rank * 128), peer_smem(smem_u32(&full[s]), 0));
       }
       dependency_wait();
       int issued = 0;
-      for (int64_t t = pair; t < tiles && ok; t += pairs) {
-        const int n0 = static_cast<int>(t / shape.token_tiles * 256 + rank * 128), m0 = static_cast<int>(t % shape.token_tiles * shape.tokens + rank * half_tokens);
+      Place place = {first_n, first_m};
+      for (int64_t t = pair; t < tiles && ok; t += pairs, place = behind(place)) {
+        const int n0 = static_cast<int>(place.n * 256 + rank * 128), m0 = static_cast<int>(place.m * shape.tokens + rank * half_tokens);
         for (int c = 0; c < chunks && ok; ++c, ++issued) {
           const int s = issued % kPairStages;
           ok = mbar_wait<true>(smem_u32(&empty[s]), (issued / kPairStages & 1) ^ 1, aborted, &g_linear_error, 111);
@@ -810,8 +823,8 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
     // what a tile's epilogue reads beside the sums is loaded during the tile before
     float sx_ahead[3], sw_ahead = 0.0f;
     T bias_ahead = {};
-    auto ahead = [&](int64_t t) {
-      const int64_t n = min(t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, a.n - 1), m0 = t % shape.token_tiles * shape.tokens;
+    auto ahead = [&](Place p) {
+      const int64_t n = min(static_cast<int64_t>(p.n) * 256 + rank * 128 + quarter * 32 + lane, a.n - 1), m0 = static_cast<int64_t>(p.m) * shape.tokens;
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
         const int j = i * 32 + lane;                        // places of the batches of 16 that start at 16 `part`, kPairStep apart
@@ -820,10 +833,12 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
       sw_ahead = a.sw[n];
       if (a.bias) bias_ahead = static_cast<const T*>(a.bias)[n];
     };
-    if (pair < tiles) ahead(pair);
+    Place place = {first_n, first_m};
+    if (pair < tiles) ahead(place);
     for (int64_t t = pair; t < tiles && ok; t += pairs, ++turn) {
       const int acc = turn & 1;
-      const int64_t n = t / shape.token_tiles * 256 + rank * 128 + quarter * 32 + lane, m0 = t % shape.token_tiles * shape.tokens;
+      const int64_t n = static_cast<int64_t>(place.n) * 256 + rank * 128 + quarter * 32 + lane, m0 = static_cast<int64_t>(place.m) * shape.tokens;
+      place = behind(place);
       const int most = static_cast<int>(min(static_cast<int64_t>(shape.tokens), a.m - m0));
       float* sx = scales[warp - 2];
       __syncwarp();
@@ -831,38 +846,37 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
       for (int i = 0; i < 3; ++i) sx[i * 32 + lane] = sx_ahead[i];
       __syncwarp();
       const float sw = sw_ahead, bias = a.bias ? Storage<T>::load1(&bias_ahead) : 0.0f;
-      if (t + pairs < tiles) ahead(t + pairs);
-      T add[16];
-      if (a.residual) residual_ahead<T, 16>(a, m0 + part * 16, n, add);
+      if (t + pairs < tiles) ahead(place);
+      T add[16], add_next[16];
+      if (RES) residual_ahead<T, 16>(a, m0 + part * 16, n, add);
       ok = mbar_wait<false>(smem_u32(&acc_full[acc]), turn >> 1 & 1, aborted, &g_linear_error, 114);
       ok = __all_sync(0xFFFFFFFFu, ok) && !*aborted;
       ok = __all_sync(0xFFFFFFFFu, ok);
       tc_fence_after();
       if (ok) {
         const uint32_t sums = mine + acc * 256;
-        uint32_t v[16];
+        uint32_t v[16], v_next[16];
         int c = part * 16;
         if (c < most) tmem_ld16(sums + c, v);
         tmem_ld_wait();
-        for (; c < most; c += kPairStep) {
-          uint32_t w[16];
-          T next[16];
+        // one batch: the sums of the next (if there is one) are on their way meanwhile, in the other registers
+        auto batch = [&](const uint32_t (&now)[16], const T (&now_add)[16], uint32_t (&next)[16], T (&next_add)[16]) {
           const bool more = c + kPairStep < most;
           if (more) {
-            tmem_ld16(sums + c + kPairStep, w);
-            if (a.residual) residual_ahead<T, 16>(a, m0 + c + kPairStep, n, next);
-          }
-          if (!more) {                                      // all of this warp's columns are in registers
+            tmem_ld16(sums + c + kPairStep, next);
+            if (RES) residual_ahead<T, 16>(a, m0 + c + kPairStep, n, next_add);
+          } else {                                          // all of this warp's columns are in registers
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(smem_u32(&acc_empty[acc]), 0));
           }
-          finish<T, DROP, 16>(a, v, sx + c / kPairStep * 16, m0 + c, n, sw, bias, add);
-          if (more) {
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = w[j], add[j] = next[j];
-          }
+          finish<T, DROP, RES, 16>(a, now, sx + c / kPairStep * 16, m0 + c, n, sw, bias, now_add);
+          if (more) tmem_ld_wait();
+          c += kPairStep;
+        };
+        while (c < most) {
+          batch(v, add, v_next, add_next);
+          if (c < most) batch(v_next, add_next, v, add);
         }
         if (part * 16 >= most) {                            // (a warp without tokens in this tile)
           __syncwarp();
@@ -915,9 +929,11 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
 }
 
 // Kernel, tokens per tile and CTAs per tile: the choice with the shortest estimate, in cycles of a multiprocessor.  From sweeps of all choices
-// at 22 sizes (5 to 8192 tokens, 512 x 512 to 5120 x 13824 and 50265 x 1027 weights): operands arrive at about 70 bytes a cycle, the tensor cores
-// do 128 * 48 products a cycle, a token of the epilogue costs 25 cycles, sums that travel between CTAs 600 a CTA and 12 a token.  One CTA on a
-// multiprocessor with all of its shared memory as stages is better than two, and pairs are better than several rounds of single CTAs.
+// at 32 sizes (5 to 8192 tokens, 512 x 512 to 5120 x 13824 and 50265 x 1027 weights, inner dimensions from 19 on): operands arrive at about 70 bytes a
+// cycle, the tensor cores do 128 * 48 products a cycle, a token of the epilogue costs 25 cycles, sums that travel between CTAs 600 a CTA and 12 a
+// token.  One CTA on a multiprocessor with all of its shared memory as stages is better than two, and pairs are better than several rounds of
+// single CTAs.  A pair's epilogue takes 930 cycles a step of its twelve warps (48 tokens) and 700 a tile; where the inner dimension is short that
+// is what a tile takes (without it small tiles were chosen: 1024 x 256 -> 50304 63 us against 41, 8192 x 512 -> 4096 45 against 29).
 constexpr int kTileSmem = 110 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
 int tile_sums_bytes(const TileShape& s) { return s.split > 1 ? (s.tokens / 16 + s.split - 1) / s.split * 16 * s.split * kTileChannels * 4 : 0; }
 // copies beside products: the longer of the two, and some of the other (both draw on the same power)
@@ -926,7 +942,7 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
   TileShape best = {};
   double least = 0;
   const int64_t channel_tiles = (n + kTileChannels - 1) / kTileChannels, chunks = (k + kChunk - 1) / kChunk;
-  for (int64_t most = 256; most >= 16; most = most == 256 ? 192 : (most == 192 ? 128 : (most == 128 ? 96 : (most == 96 ? 64 : most / 2)))) {
+  for (const int64_t most : {256, 224, 192, 160, 128, 96, 64, 32, 16}) {
     TileShape s = {};
     s.token_tiles = static_cast<int32_t>((m + most - 1) / most);
     s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
@@ -937,7 +953,7 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
       const double inner = static_cast<double>((chunks + s.split - 1) / s.split * kChunk);
       const double steady = overlapped(inner * (kTileChannels + s.tokens) / 70, inner * s.tokens / 48);
       const double ends = 3000 + 25.0 * s.tokens / s.split + (s.split > 1 ? 600 * s.split + 12.0 * s.tokens : 0);
-      const double cost = steady * each + ends * ((each + 1) / 2) + (each > 1 ? 1500 : 0);
+      const double cost = steady * each + ends * ((each + 1) / 2) + (each > 1 ? 1200.0 * each : 0);
       if (best.tokens == 0 || cost < least) {
         const int stage = (kTileChannels + s.tokens) * kChunk;
         s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024 - tile_sums_bytes(s)) / stage);
@@ -952,8 +968,9 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
       s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
       const int64_t rounds = ((n + 255) / 256 * s.token_tiles + kPairs - 1) / kPairs;
       const double inner = static_cast<double>(chunks * kChunk);
-      const double steady = overlapped(inner * (kTileChannels + s.tokens / 2) / 70, inner * s.tokens / 48);
-      const double cost = std::max(steady, 25.0 * s.tokens) * rounds + 6500 + 25.0 * s.tokens;
+      const double steady = overlapped(inner * (kTileChannels + s.tokens / 2) / 70, inner * s.tokens / 48) + 700;
+      const double epilogue = 700 + 930.0 * ((s.tokens + kPairStep - 1) / kPairStep);
+      const double cost = std::max(steady, epilogue) * rounds + 5000 + std::min(steady, epilogue);
       if (cost < least) {
         best = s;
         least = cost;
@@ -964,27 +981,31 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
 }
 int tile_smem_bytes(const TileShape& s) { return s.stages * (kTileChannels + s.tokens) * kChunk + tile_sums_bytes(s) + 1024; }
 
-template <typename T, bool DROP>
+template <typename T, bool DROP, bool RES>
 cudaError_t launch_tile(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmemAlone + 1024);
+  cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<T, DROP, RES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTileSmemAlone + 1024);
   if (e != cudaSuccess) return e;
   const int64_t ctas = (a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split;
-  return launch_behind(linear_tile_kernel<T, DROP>, static_cast<unsigned>(ctas), kTileThreads, tile_smem_bytes(s), s.split, st, mw, mx, a, s);
+  return launch_behind(linear_tile_kernel<T, DROP, RES>, static_cast<unsigned>(ctas), kTileThreads, tile_smem_bytes(s), s.split, st, mw, mx, a, s);
 }
-template <typename T, bool DROP>
+template <typename T, bool DROP, bool RES>
 cudaError_t launch_pair(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
   constexpr int smem = kPairStages * kPairStageBytes + 1024;
-  cudaError_t e = cudaFuncSetAttribute(linear_pair_kernel<T, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(linear_pair_kernel<T, DROP, RES>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (a.n + 255) / 256 * s.token_tiles;
-  return launch_behind(linear_pair_kernel<T, DROP>, static_cast<unsigned>(2 * std::min<int64_t>(tiles, kPairs)), kPairThreads, smem, 2, st, mw, mx, a, s, tiles);
+  return launch_behind(linear_pair_kernel<T, DROP, RES>, static_cast<unsigned>(2 * std::min<int64_t>(tiles, kPairs)), kPairThreads, smem, 2, st, mw, mx, a, s, tiles);
 }
 
 template <typename T>
 cudaError_t launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const LinearArgs& a, const TileShape& s, cudaStream_t st) {
   const bool drop = a.mask.threshold != 0;
-  if (s.pair) return drop ? launch_pair<T, true>(mw, mx, a, s, st) : launch_pair<T, false>(mw, mx, a, s, st);
-  return drop ? launch_tile<T, true>(mw, mx, a, s, st) : launch_tile<T, false>(mw, mx, a, s, st);
+  if (a.residual) {
+    if (s.pair) return drop ? launch_pair<T, true, true>(mw, mx, a, s, st) : launch_pair<T, false, true>(mw, mx, a, s, st);
+    return drop ? launch_tile<T, true, true>(mw, mx, a, s, st) : launch_tile<T, false, true>(mw, mx, a, s, st);
+  }
+  if (s.pair) return drop ? launch_pair<T, true, false>(mw, mx, a, s, st) : launch_pair<T, false, false>(mw, mx, a, s, st);
+  return drop ? launch_tile<T, true, false>(mw, mx, a, s, st) : launch_tile<T, false, false>(mw, mx, a, s, st);
 }
 
 // Product of codes with the tensor cores.
