@@ -499,7 +499,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const uint32_t (&sum
 }
 
 template <typename T, bool DROP, bool RES>
-__global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+__global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                                    const LinearArgs a, const TileShape shape) {
   extern __shared__ uint8_t tile_smem[];
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done;
@@ -934,7 +934,8 @@ bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, in
 // token.  One CTA on a multiprocessor with all of its shared memory as stages is better than two, and pairs are better than several rounds of
 // single CTAs.  A pair's epilogue takes 930 cycles a step of its twelve warps (48 tokens) and 700 a tile; where the inner dimension is short that
 // is what a tile takes (without it small tiles were chosen: 1024 x 256 -> 50304 63 us against 41, 8192 x 512 -> 4096 45 against 29).
-constexpr int kTileSmem = 110 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
+// (kTileSmem: two CTAs with 4304 static bytes and 1024 of the system each on a multiprocessor of 228 KB; at 110 KB 600 x 300 -> 9000 had one: 12.2 us)
+constexpr int kTileSmem = 108 * 1024, kTileSmemAlone = 215 * 1024, kPairs = 74;
 int tile_sums_bytes(const TileShape& s) { return s.split > 1 ? (s.tokens / 16 + s.split - 1) / s.split * 16 * s.split * kTileChannels * 4 : 0; }
 // copies beside products: the longer of the two, and some of the other (both draw on the same power)
 double overlapped(double a, double b) { return std::max(a, b) + 0.3 * std::min(a, b); }
@@ -950,14 +951,16 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
     for (s.split = 1; s.split <= 4 && (s.split == 1 || chunks >= 2 * s.split); s.split *= 2) {
       // (clusters of four fill 128 multiprocessors: 36 of them, 1128 x 5918 -> 256, took 15.2 us, 24 of larger tiles 9.3)
       const int64_t ctas = channel_tiles * s.token_tiles * s.split, room = s.split == 4 ? 128 : (s.split == 2 ? 144 : 148), each = (ctas + room - 1) / room;
+      const int stage = (kTileChannels + s.tokens) * kChunk;
+      s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024 - tile_sums_bytes(s)) / stage);
+      if (s.stages < 2) continue;
       const double inner = static_cast<double>((chunks + s.split - 1) / s.split * kChunk);
-      const double steady = overlapped(inner * (kTileChannels + s.tokens) / 70, inner * s.tokens / 48);
+      // (what is on its way takes some 1500 cycles: the cluster's sums may leave room for few stages; 300 x 4096 -> 4096 14.1 us with three, 11.8 by pairs)
+      const double rate = s.split > 1 ? std::min(70.0, (s.stages - 1) * stage / 1500.0) : 70.0;
+      const double steady = overlapped(inner * (kTileChannels + s.tokens) / rate, inner * s.tokens / 48);
       const double ends = 3000 + 25.0 * s.tokens / s.split + (s.split > 1 ? 600 * s.split + 12.0 * s.tokens : 0);
       const double cost = steady * each + ends * ((each + 1) / 2) + (each > 1 ? 1200.0 * each : 0);
       if (best.tokens == 0 || cost < least) {
-        const int stage = (kTileChannels + s.tokens) * kChunk;
-        s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024 - tile_sums_bytes(s)) / stage);
-        if (s.stages < 2) continue;
         best = s;
         least = cost;
       }
