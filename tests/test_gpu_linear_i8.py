@@ -305,3 +305,21 @@ def test_a_new_thread_may_begin_with_a_product_of_codes():
     t.join()
     torch.cuda.synchronize()
     assert got[0] is out and torch.equal(out, want)
+
+
+# tiles of 160 and 224 tokens by pairs, two CTAs on a multiprocessor, short inner dimensions with many tiles
+@pytest.mark.parametrize("m,k,n", [(1000, 512, 11008), (4100, 512, 4096), (600, 300, 9000), (300, 4096, 4096), (333, 256, 20000), (5000, 64, 512)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_whole_batches_and_parts_of_them_agree(m, k, n, residual):
+    x, w = make((m, k), "bf16"), make((n, k), "bf16", 1)
+    r = make((m, n), "bf16", 2) if residual else None
+    (xq, xs), (wq, ws) = zgr.quantize_rows(x), zgr.quantize_rows(w)
+    y = zgr.matmul_i8(xq, xs, wq, ws, residual=r)
+    for at in range(0, m, 40):      # (another kernel and other tiles)
+        assert torch.equal(zgr.matmul_i8(xq[at:at + 40], xs[at:at + 40], wq, ws, residual=None if r is None else r[at:at + 40]), y[at:at + 40]), at
+    rows = [0, m // 2, m - 1]
+    want = (xq[rows].double() @ wq.double().T) * xs[rows].double()[:, None] * ws.double() + (0 if r is None else r[rows].double())
+    # the sum to fp32, the product of the scales, theirs and the residual: four roundings of 2^-24 of terms; the last of 2^-8
+    size = want.abs() + (0 if r is None else 2 * r[rows].double().abs())
+    assert bool(((y[rows].double() - want).abs() <= want.abs() * 2.0 ** -8 + size * 2.0 ** -21 + 1e-30).all())
+    assert zgr.linear_status() == 0
