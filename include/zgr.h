@@ -406,6 +406,16 @@ int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8
  * that gave up since the library was loaded (0 = healthy; the call it belonged to left y unfinished). */
 int zgr_linear_status(int32_t* code);
 
+/* Test hook, as zgr_debug_plan: the kernel that serves a product of these sizes, computed on the host alone.  codes: 0 for zgr_linear_i8, else
+ * zgr_matmul_i8.  kernel: few tokens at a time, tiles of one CTA or of a cluster of `split`, tiles of pairs of CTAs; tokens: of a tile (of
+ * the call, where there are few).
+ * ZGR_EINVAL: null out, m < 1, sizes that the products refuse. */
+enum { ZGR_LINEAR_FEW = 0, ZGR_LINEAR_TILE = 1, ZGR_LINEAR_PAIR = 2 };
+typedef struct {
+  int32_t kernel, tokens, split;
+} zgr_linear_plan;
+int zgr_debug_linear_plan(int64_t m, int64_t n, int64_t k, int32_t codes, zgr_linear_plan* out);
+
 void zgr_destroy(zgr_ctx* ctx);
 const char* zgr_strerror(int code);
 

@@ -1065,10 +1065,12 @@ bool codes_ok(const int8_t* p, int64_t rows, int64_t k, int64_t ld) {
   return matrix_ok(p, rows, k, ld, 1) && aligned_to(p, 16) && (rows <= 1 || (ld % 16 == 0 && ld < (int64_t{1} << 40)));
 }
 
+bool sizes_ok(int64_t m, int64_t n, int64_t k) { return m >= 0 && n >= 1 && k >= 1 && k <= kMaxInner && m <= 0x7FFFFFFF && n <= 0x7FFFFFFF; }
+
 // Arguments of the product that both entry points check: everything but the tokens.
 bool product_ok(const int8_t* w, int64_t ldw, const float* sw, const void* bias, const void* residual, int64_t ldr, const void* y, int64_t ldy, int64_t m,
                 int64_t n, int64_t k, int32_t dtype, double p) {
-  if (!storage_known(dtype) || m < 0 || n < 1 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF || n > 0x7FFFFFFF || !(p >= 0.0 && p <= 1.0)) return false;
+  if (!storage_known(dtype) || !sizes_ok(m, n, k) || !(p >= 0.0 && p <= 1.0)) return false;
   if (m == 0) return true;
   const int size = storage_size(dtype);
   if (!codes_ok(w, n, k, ldw) || !sw || !aligned_to(sw, 4) || !aligned_to(bias, size)) return false;
@@ -1111,7 +1113,7 @@ int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, in
 }
 
 int64_t zgr_linear_i8_workspace(int64_t m, int64_t n, int64_t k) {
-  if (m < 0 || n < 1 || k < 1 || k > kMaxInner || m > 0x7FFFFFFF || n > 0x7FFFFFFF) return ZGR_EINVAL;
+  if (!sizes_ok(m, n, k)) return ZGR_EINVAL;
   return few(m, n, k) ? 0 : scales_at(m, k) + m * static_cast<int64_t>(sizeof(float));
 }
 
@@ -1146,6 +1148,17 @@ int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8
   LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
   a.sx = x_scale;
   return run_product(x, ldx, a, dtype, false, static_cast<cudaStream_t>(stream));
+}
+
+int zgr_debug_linear_plan(int64_t m, int64_t n, int64_t k, int32_t codes, zgr_linear_plan* out) {
+  if (!out || !sizes_ok(m, n, k) || m == 0) return ZGR_EINVAL;
+  if (!codes && few(m, n, k)) {
+    *out = {ZGR_LINEAR_FEW, static_cast<int32_t>(m), 1};
+  } else {
+    const TileShape s = tile_shape(m, n, k);
+    *out = {s.pair ? ZGR_LINEAR_PAIR : ZGR_LINEAR_TILE, s.tokens, s.split};
+  }
+  return ZGR_OK;
 }
 
 int zgr_linear_status(int32_t* code) {

@@ -44,6 +44,11 @@ class ZgrKernelTime(ctypes.Structure):
                 ("elements", ctypes.c_int64), ("ms_total", ctypes.c_double)]
 
 
+class LinearPlan(ctypes.Structure):
+    _fields_ = [("kernel", ctypes.c_int32), ("tokens", ctypes.c_int32), ("split", ctypes.c_int32)]
+
+
+LINEAR_FEW, LINEAR_TILE, LINEAR_PAIR = 0, 1, 2
 PATH_NAMES = {0: "iso", 1: "fma", 2: "mma", 3: "generic", 4: "umma"}
 KERNEL_NAMES = {**PATH_NAMES, 5: "tile", 6: "staged"}      # sweep_<name>_kernel
 
@@ -108,7 +113,8 @@ def lib() -> ctypes.CDLL:
         L.zgr_linear_i8.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, i64, i64, i32, dbl, u64, ctypes.c_uint32, vp, i64, vp]
         L.zgr_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, i64, i64, i64, i64, i32, dbl, u64, ctypes.c_uint32, vp]
         L.zgr_linear_status.argtypes = [ctypes.POINTER(i32)]
-        for name in ("zgr_dropout", "zgr_dropout_backward", "zgr_quantize_rows", "zgr_linear_i8", "zgr_matmul_i8", "zgr_linear_status"):
+        L.zgr_debug_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(LinearPlan)]
+        for name in ("zgr_dropout", "zgr_dropout_backward", "zgr_quantize_rows", "zgr_linear_i8", "zgr_matmul_i8", "zgr_linear_status", "zgr_debug_linear_plan"):
             getattr(L, name).restype = ctypes.c_int
         L.zgr_dropout_backward_workspace.argtypes, L.zgr_linear_i8_workspace.argtypes = [i64, i64], [i64, i64, i64]
         L.zgr_dropout_backward_workspace.restype = L.zgr_linear_i8_workspace.restype = i64
@@ -240,6 +246,13 @@ def linear_status() -> int:
     code = ctypes.c_int32()
     _check(lib().zgr_linear_status(ctypes.byref(code)), "zgr_linear_status")
     return code.value
+
+
+def debug_linear_plan(m: int, n: int, k: int, codes: bool = False):
+    """(kernel, tokens of a tile, CTAs of a tile) of a product of these sizes (zgr_debug_linear_plan); kernel is one of LINEAR_*."""
+    plan = LinearPlan()
+    _check(lib().zgr_debug_linear_plan(m, n, k, int(codes), ctypes.byref(plan)), "zgr_debug_linear_plan")
+    return plan.kernel, plan.tokens, plan.split
 
 
 class Zgr:
