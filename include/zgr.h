@@ -403,7 +403,8 @@ int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8
                   uint32_t tensor, void* stream);
 
 /* Device-side health of the two products on the current device, as zgr_device_status: synchronises and gives the code of the first wait
- * that gave up since the library was loaded (0 = healthy; the call it belonged to left y unfinished). */
+ * that gave up since the library was loaded (0 = healthy; the call it belonged to left y unfinished: what it wrote is right, other elements
+ * are as they were). */
 int zgr_linear_status(int32_t* code);
 
 /* Test hook, as zgr_debug_plan: the kernel that serves a product of these sizes, computed on the host alone.  codes: 0 for zgr_linear_i8, else
@@ -415,6 +416,12 @@ typedef struct {
   int32_t kernel, tokens, split;
 } zgr_linear_plan;
 int zgr_debug_linear_plan(int64_t m, int64_t n, int64_t k, int32_t codes, zgr_linear_plan* out);
+
+/* Test hook: zgr_matmul_i8 in which the first wait of one thread block counts as run out, which zgr_linear_status reports from then on.
+ * block: -1 for none. */
+int zgr_debug_matmul_i8_giving_up(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
+                                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p,
+                                  uint64_t seed, uint32_t tensor, int32_t block, void* stream);
 
 void zgr_destroy(zgr_ctx* ctx);
 const char* zgr_strerror(int code);

@@ -228,10 +228,12 @@ __device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
   acc = __dp4a(static_cast<int>(a.z), static_cast<int>(b.z), acc);
   return __dp4a(static_cast<int>(a.w), static_cast<int>(b.w), acc);
 }
-// What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too.
+// What is left in flight when a wait has given up: the CTA must not leave before its copies and products have landed.  Bounded too, by
+// some 70 ms: copies and products take microseconds, and a barrier that another role has given up on never completes.
+constexpr unsigned long long kDrainLimitCycles = 1ull << 27;
 __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
   const unsigned long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitLimitCycles) {
+  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kDrainLimitCycles) {
   }
 }
 
@@ -406,6 +408,7 @@ struct TileShape {
   int32_t split;         // CTAs of a cluster that share a tile
   int32_t stages;
   int32_t token_tiles;
+  int32_t give_up;       // test hook: the block whose first wait counts as run out; -1: none
   int32_t weights_ahead; // 1: the kernel in front is the tokens' quantiser, which lets this one start after its own wait: the weights are older
 };
 
@@ -435,6 +438,13 @@ __device__ __forceinline__ uint32_t peer_smem(uint32_t addr, uint32_t rank) {
   return r;
 }
 __device__ __forceinline__ void sts_peer(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+// A wait of the block that the test hook names has run out: as mbar_wait leaves it.
+__device__ __forceinline__ bool first_wait(const TileShape& shape, int* abort_flag) {
+  if (static_cast<int>(blockIdx.x) != shape.give_up) return true;
+  *static_cast<volatile int*>(abort_flag) = 1;
+  atomicCAS(&g_linear_error, 0, 100);
+  return false;
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap& map) { asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory"); }
 // The sum of a cluster's CTAs for one token and channel, from the slots that they have filled in this CTA's shared memory.
 __device__ __forceinline__ uint32_t sum_of_slots(uint32_t at, uint32_t slot_bytes, int split) {
@@ -505,6 +515,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
+  __shared__ int unfinished;      // a CTA of the cluster has no sums
   __shared__ float scales[8][128];
   const uint32_t stages0 = (smem_u32(tile_smem) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -523,7 +534,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
   if (threadIdx.x == 0) {
     prefetch_map(map_w);
     prefetch_map(map_x);
-    abort_flag = 0;
+    abort_flag = unfinished = 0;
     for (int s = 0; s < shape.stages; ++s) {
       mbar_init(smem_u32(&full[s]), 1);
       mbar_init(smem_u32(&empty[s]), 1);
@@ -550,6 +561,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
         tma_load_2d(stages0 + s * stage_bytes, &map_w, (first + s) * kChunk, static_cast<int>(n0), smem_u32(&full[s]));
       }
       dependency_wait();
+      ok = first_wait(shape, &abort_flag);
       int issued = 0;
       for (int c = first, s = 0, phase = 0; c < last && ok; ++c) {
         ok = mbar_wait<true>(smem_u32(&empty[s]), phase ^ 1, aborted, &g_linear_error, 101);
@@ -635,11 +647,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
 #pragma unroll
         for (int j = 0; j < 8; ++j) sts_peer(to + j * kTileChannels * 4, v[j]);
       }
+    } else if (warp >= 2 && lane < shape.split) {             // the sums of the whole cluster lack this CTA's: nobody writes results of them
+      sts_peer(peer_smem(smem_u32(&unfinished), lane), 1);
     }
     __syncwarp();
     cluster_arrive();
     cluster_wait();
-    if (warp >= 2) {
+    if (warp >= 2 && *static_cast<volatile int*>(&unfinished) == 0) {
       for (int place = half; place < own_groups; place += 2) {
         const int g = ((place >> 1) * shape.split + static_cast<int>(rank)) * 2 + (place & 1);
         if (g >= groups || m0 + g * 8 >= a.m) break;
@@ -734,6 +748,13 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
     return p;
   };
   volatile int* aborted = &abort_flag;
+  // A producer or issuer whose wait gave up ends the work of both CTAs: the other one must not take an accumulator that lacks products for a
+  // good one.  (In front of whatever this role still signals; nobody has left by then, because of the barrier at the end.)
+  auto give_up = [&] {
+    *aborted = 1;
+    sts_peer(peer_smem(smem_u32(&abort_flag), rank ^ 1), 1);
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  };
   if (threadIdx.x == 0) {
     prefetch_map(map_w);
     prefetch_map(map_x);
@@ -760,7 +781,6 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
   const uint32_t tmem = tmem_slot;
   if (warp == 0) {
     if (elect_one()) {
-      bool ok = true;
       // weights before the wait, as in linear_tile_kernel
       const int ahead = shape.weights_ahead ? min(kPairStages, chunks) : 0, stage_bytes = (kTileChannels + half_tokens) * kChunk;
       for (int s = 0; s < ahead; ++s) {
@@ -768,6 +788,7 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
         tma_load_pair(stages0 + s * kPairStageBytes, &map_w, s * kChunk, static_cast<int>(first_n * 256 + rank * 128), peer_smem(smem_u32(&full[s]), 0));
       }
       dependency_wait();
+      bool ok = first_wait(shape, &abort_flag);
       int issued = 0;
       Place place = {first_n, first_m};
       for (int64_t t = pair; t < tiles && ok; t += pairs, place = behind(place)) {
@@ -784,9 +805,15 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
           tma_load_pair(at + kTileChannels * kChunk, &map_x, c * kChunk, m0, bar);
         }
       }
-      // as in linear_tile_kernel (the even CTA's barriers count the copies of both)
-      for (int c = max(0, issued - kPairStages); c < issued && (ok || rank == 0); ++c)
-        mbar_drain(smem_u32(ok ? &empty[c % kPairStages] : &full[c % kPairStages]), c / kPairStages & 1);
+      if (ok) {
+        // as in linear_tile_kernel
+        for (int c = max(0, issued - kPairStages); c < issued; ++c) mbar_drain(smem_u32(&empty[c % kPairStages]), c / kPairStages & 1);
+      } else {
+        // The even CTA's barriers count the copies of both, and no longer all of them: time for the copies in flight instead.
+        give_up();
+        const unsigned long long t0 = clock64();
+        while (clock64() - t0 < kDrainLimitCycles) __nanosleep(1000);
+      }
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -809,6 +836,7 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
           for (int i = 0; i < kChunk / 32; ++i) umma_i8_pair(tmem + acc * 256, wdesc + 2 * i, xdesc + 2 * i, idesc, c > 0 || i > 0);
           umma_commit_pair(smem_u32(&empty[s]));
         }
+        if (!ok) give_up();
         umma_commit_pair(smem_u32(&acc_full[acc]));
         if (!ok) mbar_drain(smem_u32(&acc_full[acc]), turn >> 1 & 1);
       }
@@ -1012,8 +1040,9 @@ cudaError_t launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const L
 }
 
 // Product of codes with the tensor cores.
-int run_product(const int8_t* xq, int64_t ldq, const LinearArgs& a, int32_t dtype, bool behind_quantiser, cudaStream_t st) {
+int run_product(const int8_t* xq, int64_t ldq, const LinearArgs& a, int32_t dtype, bool behind_quantiser, cudaStream_t st, int give_up = -1) {
   TileShape s = tile_shape(a.m, a.n, a.k);
+  s.give_up = give_up;
   s.weights_ahead = behind_quantiser;
   if ((a.n + kTileChannels - 1) / kTileChannels * s.token_tiles * s.split > 0x7FFFFFFF) return ZGR_ETOOBIG;
   CUtensorMap mw, mx;
@@ -1139,15 +1168,21 @@ int zgr_linear_i8(const void* x, int64_t ldx, const int8_t* w, int64_t ldw, cons
   return run_product(codes, padded(k), a, dtype, true, st);
 }
 
-int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
-                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed,
-                  uint32_t tensor, void* stream) {
+int zgr_debug_matmul_i8_giving_up(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
+                                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p,
+                                  uint64_t seed, uint32_t tensor, int32_t block, void* stream) {
   if (!product_ok(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p)) return ZGR_EINVAL;
   if (m == 0) return ZGR_OK;
   if (!codes_ok(x, m, k, ldx) || !x_scale || !aligned_to(x_scale, 4) || static_cast<const void*>(x) == y) return ZGR_EINVAL;
   LinearArgs a = linear_args(w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, p, seed, tensor);
   a.sx = x_scale;
-  return run_product(x, ldx, a, dtype, false, static_cast<cudaStream_t>(stream));
+  return run_product(x, ldx, a, dtype, false, static_cast<cudaStream_t>(stream), block);
+}
+
+int zgr_matmul_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, const void* bias,
+                  const void* residual, int64_t ldr, void* y, int64_t ldy, int64_t m, int64_t n, int64_t k, int32_t dtype, double p, uint64_t seed,
+                  uint32_t tensor, void* stream) {
+  return zgr_debug_matmul_i8_giving_up(x, ldx, x_scale, w, ldw, w_scale, bias, residual, ldr, y, ldy, m, n, k, dtype, p, seed, tensor, -1, stream);
 }
 
 int zgr_debug_linear_plan(int64_t m, int64_t n, int64_t k, int32_t codes, zgr_linear_plan* out) {

@@ -112,9 +112,11 @@ def lib() -> ctypes.CDLL:
         L.zgr_quantize_rows.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
         L.zgr_linear_i8.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, i64, i64, i32, dbl, u64, ctypes.c_uint32, vp, i64, vp]
         L.zgr_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, i64, i64, i64, i64, i32, dbl, u64, ctypes.c_uint32, vp]
+        L.zgr_debug_matmul_i8_giving_up.argtypes = L.zgr_matmul_i8.argtypes[:-1] + [i32, vp]
         L.zgr_linear_status.argtypes = [ctypes.POINTER(i32)]
         L.zgr_debug_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(LinearPlan)]
-        for name in ("zgr_dropout", "zgr_dropout_backward", "zgr_quantize_rows", "zgr_linear_i8", "zgr_matmul_i8", "zgr_linear_status", "zgr_debug_linear_plan"):
+        for name in ("zgr_dropout", "zgr_dropout_backward", "zgr_quantize_rows", "zgr_linear_i8", "zgr_matmul_i8", "zgr_linear_status", "zgr_debug_linear_plan",
+                     "zgr_debug_matmul_i8_giving_up"):
             getattr(L, name).restype = ctypes.c_int
         L.zgr_dropout_backward_workspace.argtypes, L.zgr_linear_i8_workspace.argtypes = [i64, i64], [i64, i64, i64]
         L.zgr_dropout_backward_workspace.restype = L.zgr_linear_i8_workspace.restype = i64
