@@ -7,6 +7,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -43,10 +44,18 @@ const at::Tensor& tensor_of(PyObject* o, const char* what) {
   return THPVariable_Unpack(o);
 }
 
+// The current device, and whether autograd would record a call: these record nothing, so a result would be a constant to the backward pass, and an
+// output that requires gradients would keep the history of its old values.  Refused, unless the caller has switched recording off.
 struct Here {
   int device;
-  Here() : device(c10::cuda::current_device()) {}
+  bool recording;
+  Here() : device(c10::cuda::current_device()), recording(c10::GradMode::is_enabled()) {}
   void check(const at::Tensor& t, const char* what) const {
+    dense(t, what);
+    if (recording && t.requires_grad())
+      throw Refused(std::string(what) + " requires gradients, which this call does not record: call it under torch.no_grad(), or pass it detached");
+  }
+  void dense(const at::Tensor& t, const char* what) const {
     if (!t.is_cuda() || t.get_device() != device) throw Refused(std::string(what) + " must be on the current CUDA device");
     if (t.layout() != at::kStrided) throw Refused(std::string(what) + " must be a dense tensor");
     if (t.is_neg()) throw Refused(std::string(what) + " must not be a view whose sign is still to be changed (resolve_neg)");
@@ -217,7 +226,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject* {
     const Here here;
     const at::Tensor& x = tensor_of(a[0], "x");
-    here.check(x, "x");
+    here.dense(x, "x");      // (weights that are parameters are quantised as they are: codes are whole numbers, which have no gradient)
     const int storage = storage_of(x.scalar_type(), "x");
     if (x.dim() != 2) throw Refused("x must be a matrix");
     const Matrix m = matrix_of(x, "x");

@@ -158,7 +158,8 @@ def _stream_ptr(stream) -> Optional[int]:
 # -- operators of the forward pass --------------------------------------------------------------------------------
 # Their marshalling is a compiled module (csrc/zgr_bind.cpp), built beside the library: they last a few microseconds on the device, and
 # ctypes with the checks around it took as long.  It calls the functions of the library loaded above.  Nothing here is recorded by
-# autograd: the backward pass is a call of its own, under the same (p, seed, tensor).
+# autograd: the backward pass is a call of its own, under the same (p, seed, tensor), and a tensor that requires gradients is refused while
+# autograd records (ValueError), rather than its gradient lost without a word.
 _STORAGE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _bind = None
 
@@ -188,7 +189,8 @@ def _on_stream(f, stream, *args):
 
 def dropout(x, p: float, seed: int, tensor: int = 0, bias=None, residual=None, out=None, stream=None):
     """residual + dropout(x + bias) with the mask of (seed, tensor), which is never stored (zgr_dropout).  x: (..., cols), its last
-    dimension contiguous; residual and out: of the same shape; out may be x or residual itself.  Returns out."""
+    dimension contiguous; residual and out: of the same shape; out may be x or residual itself.  Returns out.  Autograd does not record
+    it: tensors that require gradients are taken under torch.no_grad() only, and `dropout_backward` is the gradient."""
     f = (_bind or _load_bind()).dropout
     r = f(x, p, seed, tensor, bias, residual, out) if stream is None else _on_stream(f, stream, x, p, seed, tensor, bias, residual, out)
     if r.__class__ is int:
@@ -207,9 +209,10 @@ def dropout_backward(dy, p: float, seed: int, tensor: int = 0, bias_grad: bool =
 
 
 def quantize_rows(x, pitch: Optional[int] = None, stream=None):
-    """Signed 8-bit codes of the rows of x (rows, cols) with a scale each (zgr_quantize_rows).  Returns (codes, scales); rows of codes
-    are `pitch` bytes apart, by default the next multiple of 128 (of 16 below 512 columns): the products want a multiple of 16 and are
-    faster where rows are whole lines; pitch = cols gives contiguous codes, which set_coeffs_dtc wants."""
+    """Signed 8-bit codes of the rows of x (rows, cols) with a scale each (zgr_quantize_rows).  Returns (codes, scales), constants to
+    autograd even where x requires gradients (weights that are parameters).  Rows of codes are `pitch` bytes apart, by default the next
+    multiple of 128 (of 16 below 512 columns): the products want a multiple of 16 and are faster where rows are whole lines;
+    pitch = cols gives contiguous codes, which set_coeffs_dtc wants."""
     f = (_bind or _load_bind()).quantize_rows
     r = f(x, pitch) if stream is None else _on_stream(f, stream, x, pitch)
     if r.__class__ is int:
@@ -220,7 +223,7 @@ def quantize_rows(x, pitch: Optional[int] = None, stream=None):
 def linear_i8(x, w, w_scale, bias=None, residual=None, p: float = 0.0, seed: int = 0, tensor: int = 0, out=None, stream=None):
     """residual + dropout(x w^T + bias) in 8 bits (zgr_linear_i8): x (..., k) is quantised with a scale for each token, w (n, k) and
     w_scale (n) are the codes and scales that quantize_rows makes of the weights.  Returns (..., n) of x's type; out may be the residual
-    itself, not x."""
+    itself, not x.  Not recorded by autograd: tensors that require gradients are taken under torch.no_grad() only."""
     f = (_bind or _load_bind()).linear_i8
     r = (f(x, w, w_scale, bias, residual, p, seed, tensor, out) if stream is None
          else _on_stream(f, stream, x, w, w_scale, bias, residual, p, seed, tensor, out))
