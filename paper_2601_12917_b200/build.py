@@ -1,7 +1,8 @@
-"""Build the CUDA library ``libzgr.so`` in-tree with nvcc for sm_100a, and beside it ``_zgr_bind.so``, the marshalling of the
-forward-pass operators from torch tensors."""
+"""Build the CUDA library ``libzgr.so`` in-tree with nvcc for sm_100a, and beside it ``_zgr_bind-<torch>-<python>.so``, the marshalling of
+the forward-pass operators from torch tensors."""
 from __future__ import annotations
 
+import importlib.metadata
 import importlib.util
 import os
 import subprocess
@@ -12,9 +13,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libzgr.so")
-BIND = os.path.join(_HERE, "_zgr_bind.so")
 SOURCES = ["zgr_dropout.cu", "zgr_host.cu", "zgr_kernels.cu", "zgr_linear.cu", "zgr_noalloc.cu", "zgr_staged.cu", "zgr_subspace.cu", "zgr_tile.cu", "zgr_umma.cu"]
 BIND_SOURCE = "zgr_bind.cpp"
+
+
+def bind_path() -> str:
+    """The marshalling module of this torch and this Python.  Their versions are in its name: it is compiled against torch's C++ headers, and
+    one that was built for another torch would misread its tensors without a word."""
+    return os.path.join(_HERE, f"_zgr_bind-{importlib.metadata.version('torch')}-{sys.implementation.cache_tag}.so")
 
 
 def _newest(paths) -> float:
@@ -38,7 +44,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd += [os.path.join(CSRC, s) for s in SOURCES]
         subprocess.run(cmd, check=True)
         os.replace(tmp, LIB)
-    if force or not _current(BIND, [os.path.join(CSRC, BIND_SOURCE), header]):
+    if force or not _current(bind_path(), [os.path.join(CSRC, BIND_SOURCE), header]):
         _build_bind()
     return LIB
 
@@ -46,13 +52,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
 def _build_bind() -> None:
     torch = os.path.dirname(importlib.util.find_spec("torch").origin)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-    tmp = BIND + f".tmp{os.getpid()}"
+    bind = bind_path()
+    tmp = bind + f".tmp{os.getpid()}"
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=1",
                     "-isystem", os.path.join(torch, "include"), "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
                     "-isystem", os.path.join(cuda, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(_ROOT, "include"),
                     os.path.join(CSRC, BIND_SOURCE), "-o", tmp, "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"],
                    check=True)
-    os.replace(tmp, BIND)
+    os.replace(tmp, bind)
 
 
 if __name__ == "__main__":

@@ -14,6 +14,8 @@ from typing import List, Optional, Sequence
 
 import torch
 
+from .build import bind_path
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("ZGR_LIBRARY", os.path.join(_HERE, "libzgr.so"))   # override: an alternative build of the same ABI
 
@@ -167,9 +169,9 @@ _bind = None
 def _load_bind():
     global _bind
     L = lib()
-    path = os.path.join(_HERE, "_zgr_bind.so")
+    path = bind_path()
     if not os.path.exists(path):
-        raise ImportError(f"{path} is missing: build it with `python -m paper_2601_12917_b200.build`")
+        raise ImportError(f"{path} is missing (it is built for one version of torch and Python): build it with `python -m paper_2601_12917_b200.build`")
     spec = importlib.util.spec_from_file_location("_zgr_bind", path)
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
