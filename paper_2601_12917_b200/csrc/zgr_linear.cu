@@ -515,7 +515,6 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
   __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], done;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  __shared__ int unfinished;      // a CTA of the cluster has no sums
   __shared__ float scales[8][128];
   const uint32_t stages0 = (smem_u32(tile_smem) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -534,7 +533,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
   if (threadIdx.x == 0) {
     prefetch_map(map_w);
     prefetch_map(map_x);
-    abort_flag = unfinished = 0;
+    abort_flag = 0;
     for (int s = 0; s < shape.stages; ++s) {
       mbar_init(smem_u32(&full[s]), 1);
       mbar_init(smem_u32(&empty[s]), 1);
@@ -648,12 +647,13 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
         for (int j = 0; j < 8; ++j) sts_peer(to + j * kTileChannels * 4, v[j]);
       }
     } else if (warp >= 2 && lane < shape.split) {             // the sums of the whole cluster lack this CTA's: nobody writes results of them
-      sts_peer(peer_smem(smem_u32(&unfinished), lane), 1);
+      sts_peer(peer_smem(smem_u32(&abort_flag), lane), 1);
     }
     __syncwarp();
     cluster_arrive();
     cluster_wait();
-    if (warp >= 2 && *static_cast<volatile int*>(&unfinished) == 0) {
+    if (warp >= 2) {
+      const int lacking = *aborted;                           // set here or by a CTA that had no sums to send
       for (int place = half; place < own_groups; place += 2) {
         const int g = ((place >> 1) * shape.split + static_cast<int>(rank)) * 2 + (place & 1);
         if (g >= groups || m0 + g * 8 >= a.m) break;
@@ -665,7 +665,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
         uint32_t sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = sum_of_slots(sums0 + (place * 8 + j) * kTileChannels * 4 + channel, slot_bytes, shape.split);
-        finish<T, DROP, RES, 8>(a, sum, sx, m0 + g * 8, n, sw, bias, add);
+        finish<T, DROP, RES, 8>(a, sum, sx, m0 + g * 8, lacking ? a.n : n, sw, bias, add);      // (nothing is stored from the n-th channel on)
       }
     }
   }
