@@ -382,7 +382,9 @@ int zgr_dropout_backward(const void* dy, int64_t lddy, void* dx, int64_t lddx, v
 int zgr_quantize_rows(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, int8_t* codes, int64_t ldc, float* scales, void* stream);
 
 /* Linear layer in 8 bits, with a scale for each token and each channel:
- *     y[t][c] = residual[t][c] + D( (sum_k qx[t][k] w[c][k]) * (sx[t] w_scale[c]) + bias[c] )       (the product of the scales in fp32)
+ *     y[t][c] = residual[t][c] + D( (sum_k qx[t][k] w[c][k]) * (sx[t] w_scale[c]) + bias[c] )
+ * The product of the scales is an fp32 number: where it is below 2^-126 the result has fewer bits, where it passes 2^128 it is infinite or
+ * NaN (rows whose largest magnitudes have a product below 2^-112 or above 2^141).
  * qx, sx: the m x k tokens x quantised as by zgr_quantize_rows; w, w_scale: n x k codes and n scales, as zgr_quantize_rows makes them
  * of the weights (after a sweep: of the perturbed ones).  D is the dropout of zgr_dropout with cols = n (p = 0: nothing).
  * The sums are exact.  A token that holds an infinity or a NaN gives NaN in its row (where it is not dropped).

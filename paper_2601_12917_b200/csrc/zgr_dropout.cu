@@ -4,8 +4,8 @@
 //   backward   dx = keep ? dy * s : 0,   dbias = column sums of dx before it is rounded
 //
 // Arithmetic in fp32, one rounding to the storage type.  A dropped element contributes nothing, whatever it holds: it is selected away,
-// not multiplied by zero.  The bound is memory: x (and residual) read once, y written once; a generator block (about 50 issue slots)
-// serves eight elements.
+// not multiplied by zero.  The bound is memory: x (and residual) read once, y written once; a generator block (about 40 issue slots
+// of a warp) serves eight elements.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -142,7 +142,9 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
 // eight elements wherever a row ends, so that all accesses are whole and aligned; a piece from column c on takes its bits from the block
 // of c, made here, from the next piece's, got from the next lane, and, where the row ends within it, sometimes from a third, made by that lane
 // alone.  fp16, 16336 x 1021: 27.8 us by the rows' own pieces (dropout_shifted_kernel), whose ends are loaded and stored element by element.
-// Index: 32 bits where the tensor has fewer than 2^31 elements: 16.1 us (4.1 TB/s) against 21.1; issue slots are what bounds it.
+// Index: 32 bits where the tensor has fewer than 2^31 elements: 16.0 us (4.2 TB/s) against 21.1.  Its 176 instructions a warp and octet are about 10 us
+// of issue and its bytes 10.3 of memory; with 43 % of the warps' places taken and every thread loading, computing and storing once, the two
+// hardly overlap, and that is what bounds it (issue slots are 52 % busy).
 template <typename T, int U, typename Index>
 __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid_constant__ DropArgs<T> a) {
   const int lane = threadIdx.x & 31, cols = static_cast<int>(a.cols);
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(kThreads) dropout_unbroken_kernel(const __grid
 // Rows that do not start on 16-byte boundaries, all matrices alike.  A row's pieces of eight elements then begin `s`
 // elements before it, at the boundary, and take the last s bits of one generator block and the first 8 - s of the next: a thread
 // makes the block of its own piece and gets its neighbour's bits from the neighbouring lane; a warp's pieces follow each other, so that only its
-// first lane makes a second block, once for U pieces.
+// first lane makes a second block, once for U pieces.  8192 x 4096 bf16 with a residual, all of them two elements off: 54 us (whole octets: 30).
 template <typename T, int U, typename Index>
 __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_constant__ DropArgs<T> a) {
   constexpr int kPhases = 16 / sizeof(T);
@@ -300,8 +302,8 @@ __global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const __grid_
 
 // Matrices whose rows start at different places of their 16-byte granules: a group of G lanes (32, or fewer where a row has fewer octets)
 // takes 8 G elements of a row.  Lane l makes the block of octet l; then lane l serves the elements l, l + G, ... , so that the accesses of a group
-// are contiguous whatever
-// their alignment, and gets the mask of each from the lane that made it.
+// are contiguous whatever their alignment, and gets the mask of each from the lane that made it.  Bound by its element-wise accesses: 8192 x 4096
+// bf16 with a residual 90 us, where rows that lie alike take 54 (dropout_shifted_kernel) and whole octets 30.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_constant__ DropArgs<T> a) {
   const int lane = threadIdx.x & 31, G = a.group, l = lane & (G - 1);
@@ -378,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 4) dropout_columns_kernel(const __gr
         py += y_step;
         block += block_step;
       };
-      int n = row0 < end ? static_cast<int>((end - row0 + row_lanes - 1) / row_lanes) : 0;      // (a range has at most 2^31 rows: the grid has its other dimension)
+      int n = row0 < end ? static_cast<int>((end - row0 + row_lanes - 1) / row_lanes) : 0;      // (a thread's rows: a range of more than 2^31 of them for each of its 8 to 256 row lanes is more than any memory holds)
       for (; n >= kRowsInFlight; n -= kRowsInFlight) {
         Octet<T> x[kRowsInFlight];
 #pragma unroll

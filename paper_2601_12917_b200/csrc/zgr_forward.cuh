@@ -138,7 +138,8 @@ __device__ __forceinline__ void Octet<__nv_bfloat16>::unpack(float (&v)[8]) cons
   }
 }
 
-// n / d for n < 2^31 by a multiplication (the operands of the launch are fixed, the division is made for every octet).
+// n / d for n < 2^31 by a multiplication (the operands of the launch are fixed, the division is made for every octet): Granlund and Montgomery,
+// "Division by invariant integers using multiplication" (1994), their unsigned form; below 2^31 its sum does not pass 32 bits.
 struct FastDiv {
   uint32_t d, mul, shift;
 };

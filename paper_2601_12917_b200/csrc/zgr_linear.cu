@@ -1,6 +1,8 @@
 // The linear layer of the forward pass in 8 bits: rows quantised with a scale each, the matrix product of two such matrices, and its epilogue.
 //
 //   quantise   a = max_k |x_k|,  scale = a (1/127),  code_k = rint(x_k (127 (1/a)))        per row (a token, or a channel's weights)
+//              (products with fp32 reciprocals by definition; quotients give another code to 4 of 10 million fp32 and 2 of 100 000 16-bit normals,
+//              all within 127 * 3.01 * 2^-24 of a border between two codes)
 //   product    y[m][n] = residual[m][n] + D( (sum_k qx[m][k] qw[n][k]) * (sx[m] sw[n]) + bias[n] ),   D: dropout, or nothing
 //
 // The sums are 32-bit integers and exact; everything behind them is fp32, rounded once to the storage type.
@@ -684,7 +686,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const __gr
 // of a tile runs beside the products of the next.
 // Barriers: full (of the even CTA) counts the bytes of both CTAs' copies; empty and acc_full are signalled in both CTAs by the even one's
 // commits; acc_empty (of the even CTA) counts the epilogue warps of both.
-// 8192 x 4096 -> 11008: 220 us, 3360 TOP/s, the tensor pipe 89 % active at the board's power cap.  Where k or the number of tokens is small,
+// 8192 x 4096 -> 11008: 220 us, 3360 TOP/s, the tensor pipe 89 % active, for the kernel alone in short runs; with its quantiser in a program, at the
+// board's power cap, the call takes 280.  Where k or the number of tokens is small,
 // operands from L2 bound it (about 65 bytes a cycle and multiprocessor): 1024 x 8192 -> 2048 takes 15.5 us, 10 at the rate above.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPairStages = 6, kPairStageBytes = 2 * kTileChannels * kChunk;
@@ -977,7 +980,9 @@ TileShape tile_shape(int64_t m, int64_t n, int64_t k) {
     s.tokens = static_cast<int32_t>(((m + s.token_tiles - 1) / s.token_tiles + 15) / 16 * 16);
     s.token_tiles = static_cast<int32_t>((m + s.tokens - 1) / s.tokens);
     for (s.split = 1; s.split <= 4 && (s.split == 1 || chunks >= 2 * s.split); s.split *= 2) {
-      // (clusters of four fill 128 multiprocessors: 36 of them, 1128 x 5918 -> 256, took 15.2 us, 24 of larger tiles 9.3)
+      // (clusters of four fill 128 multiprocessors: 36 of them, 1128 x 5918 -> 256, took 15.2 us, 24 of larger tiles 9.3.  By the occupancy
+      // calculation, with one CTA on a multiprocessor, the chip holds 33 clusters of four and 74 of two, which is what the resident pairs count
+      // on; the estimate leaves one and two of them free.)
       const int64_t ctas = channel_tiles * s.token_tiles * s.split, room = s.split == 4 ? 128 : (s.split == 2 ? 144 : 148), each = (ctas + room - 1) / room;
       const int stage = (kTileChannels + s.tokens) * kChunk;
       s.stages = std::min(kMaxStages, ((each > 1 ? kTileSmem : kTileSmemAlone) - 1024 - tile_sums_bytes(s)) / stage);
