@@ -173,23 +173,6 @@ int kshift_for(double cb) {
   return std::min(std::max(k, -24), 40);
 }
 
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// cuTensorMapEncodeTiled through the runtime (the library does not link against libcuda).
-EncodeTiledFn encode_tiled_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static bool tried = false;
-  if (!tried) {
-    tried = true;
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(ptr);
-  }
-  return fn;
-}
-
 // 2-D map over a row-major matrix of elements of `bytes` (2 or 4) bytes, rows `pitch` elements apart, box = box_cols x box_rows,
 // swizzle matching the box's row length in bytes (32, 64 or 128).
 bool make_map(CUtensorMap* out, const void* base, int bytes, int64_t rows, int64_t cols, int64_t pitch, int box_rows, int box_cols) {
@@ -1049,6 +1032,16 @@ std::vector<Group>& multi_groups(zgr_ctx* ctx, int n, int* rc) {
 }  // namespace
 
 namespace zgr {
+
+EncodeTiledFn encode_tiled_fn() {
+  static const EncodeTiledFn fn = [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return found ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
+  }();
+  return fn;
+}
 PhiloxKeys host_make_keys(uint64_t seed) { return make_keys(seed); }
 NormalScale host_make_scale(double s, int bits) { return make_scale(s, bits); }
 bool host_ctx_view(const zgr_ctx* ctx, int32_t l, TensorDesc* desc, double* a, double* b, int* bits, int* sticky, int* device) {

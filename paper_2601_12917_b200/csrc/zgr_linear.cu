@@ -13,6 +13,7 @@
 
 #include "zgr.h"
 #include "zgr_forward.cuh"
+#include "zgr_host_internal.h"
 #include "zgr_tcgen05.cuh"
 
 namespace zgr {
@@ -930,20 +931,9 @@ __global__ void __launch_bounds__(kPairThreads) linear_pair_kernel(const __grid_
 // ---------------------------------------------------------------------------------------------
 // Host.
 // ---------------------------------------------------------------------------------------------
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_fn() {
-  static const EncodeTiledFn fn = [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
-    return found ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
-  }();
-  return fn;
-}
 // Rows of codes, k of them, `pitch` bytes apart; a box is box_rows x 128 bytes, swizzled; what lies outside reads as zero.
 bool codes_map(CUtensorMap* out, const int8_t* base, int64_t rows, int64_t k, int64_t pitch, int box_rows) {
-  const EncodeTiledFn fn = encode_fn();
+  const EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(rows > 1 ? pitch : (k + 15) / 16 * 16)};
