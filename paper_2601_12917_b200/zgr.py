@@ -182,11 +182,21 @@ def _load_bind():
 
 
 def _on_stream(f, stream, *args):
-    """The call on another stream than the current one: outputs and workspaces then belong to that stream, as torch keeps account of them."""
+    """The call on another stream than the current one: outputs and workspaces then belong to that stream, as torch keeps account of them.
+    Torch is told of the other uses too: the memory of an input that the caller lets go of is not given out again before this stream has read it,
+    nor that of a result before the current stream has.  What has to be ready when is the caller's to order, as with any work on two streams."""
     if stream.device.index != torch._C._cuda_getDevice():
         raise ValueError("stream must be one of the current CUDA device")
+    here = torch.cuda.current_stream()
     with torch.cuda.stream(stream):
-        return f(*args)
+        r = f(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    for t in r if r.__class__ is tuple else (r,):
+        if isinstance(t, torch.Tensor):
+            t.record_stream(here)
+    return r
 
 
 def dropout(x, p: float, seed: int, tensor: int = 0, bias=None, residual=None, out=None, stream=None):
