@@ -351,13 +351,21 @@ class Zgr:
         _check(lib().zgr_build_subspace(self._h, tensor, ptr, host, _stream_ptr(stream)), "zgr_build_subspace")
 
     # -- compressed coefficients ----------------------------------------------------------------
+    @staticmethod
+    def _whole_rows(*tensors) -> None:
+        for t in tensors:
+            if t is not None and not t.is_contiguous():
+                raise ValueError("codes, scales and zero points must be contiguous (quantize_rows: pitch = the number of columns)")
+
     def set_coeffs_dtc(self, tensor: int, q, scale, zero=None, bits: int = 8) -> None:
+        self._whole_rows(q, scale, zero)
         self._keep.append((q, scale, zero))
         _check(lib().zgr_set_coeffs_dtc(self._h, tensor, q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), bits),
                "zgr_set_coeffs_dtc")
 
     def set_coeffs_dtc_rows(self, tensor: int, q, scale, zero, bits: int, n_rows: int) -> None:
         """Only the first n_rows rows of the tensor's coefficients come from codes (zgr_set_coeffs_dtc_rows)."""
+        self._whole_rows(q, scale, zero)
         self._keep.append((q, scale, zero))
         _check(lib().zgr_set_coeffs_dtc_rows(self._h, tensor, q.data_ptr(), scale.data_ptr(), None if zero is None else zero.data_ptr(), bits, n_rows),
                "zgr_set_coeffs_dtc_rows")
