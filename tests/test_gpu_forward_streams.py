@@ -5,7 +5,7 @@ import torch
 from paper_2601_12917_b200 import zgr
 
 pytestmark = pytest.mark.gpu
-DELAY = 50_000_000      # cycles, some 25 ms
+DELAY = 400_000_000      # cycles, some 0.2 s: longer than a busy host takes between two calls
 
 
 def normal(*shape, seed=0):
